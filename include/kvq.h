@@ -522,6 +522,164 @@ int32_t kvq_decode_attention_planned(const kvq_config* cfg, int32_t layer, const
                                      size_t workspace_bytes, void* stream);
 
 /*
+ * A prompt that goes on: a chunk of new tokens per sequence, behind whatever the sequence's cache holds (a system
+ * prompt shared by requests, the earlier chunks of a long prompt, the turns of a conversation).  The paper fills its
+ * cache from whole prompts and single tokens; these calls take any number of tokens at once: rotate the chunk's
+ * queries and Keys (kvq_rope_axes), attend (kvq_prompt_attention), take the chunk up (kvq_extend).
+ *
+ * kvq_chunk says which rows of a packed array [total][...] are whose.
+ *   starts     : device int32 [batch + 1], 4-byte aligned, ascending: sequence b's new tokens are rows starts[b] ..
+ *                starts[b+1] - 1 (none: starts[b+1] == starts[b]).  NULL: every sequence has max_tokens tokens,
+ *                sequence b's from row b * max_tokens on; total is batch * max_tokens then
+ *   total      : rows of the packed arrays, 1 .. 2^31 - 1
+ *   max_tokens : upper bound of the tokens of one sequence, 1 .. total (sizes the launches; of a longer sequence the
+ *                first max_tokens tokens are taken)
+ * The kernels clamp starts to [0, total], so a corrupt array gives wrong results, no access outside the arrays.  Rows
+ * that belong to no sequence are neither read nor written.
+ */
+typedef struct kvq_chunk {
+  const int32_t* starts;
+  int32_t total;
+  int32_t max_tokens;
+} kvq_chunk;
+
+/*
+ * Attention of every new token over its sequence's cache and, causally, over the new tokens themselves (Eq. 1 with the
+ * sets of kvq_decode_attention: quantized tokens that live in no pool, both pools' members, ring rows; then the new
+ * tokens up to the query's own, in full precision: Method, prefill phase).  On an empty cache this is the attention of
+ * a prompt.  The cache is read only and the new rows join it nowhere (kvq_extend does that).
+ *   q          : device fp16, token i of the packed array at element offset i * q_stride, its q_heads rows of head_dim
+ *                behind each other; 16-byte aligned; q_stride >= q_heads * head_dim, a multiple of 8
+ *   k_new, v_new : device fp16, token i's kv_heads rows at element offset i * kv_stride; 16-byte aligned; kv_stride >=
+ *                kv_heads * head_dim, a multiple of 8.  (q, k_new and v_new may be parts of one projection's output.)
+ *                Both NULL: no new tokens, every query sees the whole cache and nothing else (cross attention to an
+ *                encoder's states); kv_stride is ignored
+ *   seq_state  : as in kvq_decode_attention_ragged, with n_quant and n_res upper bounds of the sequences' (longer ones
+ *                are truncated to them) and res_start ignored; `active` plays no part.  NULL: n_quant, res_start and n_res are
+ *                the state of every sequence.  n_quant a multiple of group_k, <= max_seq; n_res <= res_rows; res_start
+ *                in [0, res_rows)
+ *   qcache, res, pool : as in kvq_decode_attention; slots and ring rows that hold no token may hold anything
+ *   out        : device fp16 [total][q_heads][head_dim], 8-byte aligned, not overlapping the inputs.  A query that
+ *                sees no token at all (no new tokens, empty cache) gets zeros
+ *   workspace  : at least kvq_prompt_workspace_bytes of the same cfg, max_tokens, n_quant and n_res (host only; it may be
+ *                0: then NULL will do; a negative kvq_status for arguments that are not supported), 256-byte aligned.
+ *                Its contents on entry do not matter.  Two calls that overlap in time must not share it
+ *   Range      : rows of Keys and Values that a query sees must be finite (a Key or Value that is not makes outputs
+ *                of queries that see it infinite or NaN).  New tokens behind a query's own may hold anything: they do not
+ *                change its output
+ *   Rounding   : the dequantized rows and the softmax weights are rounded to fp16 for the matrix products, which, like
+ *                the softmax's maxima and sums, are fp32
+ */
+int64_t kvq_prompt_workspace_bytes(const kvq_config* cfg, int32_t max_tokens, int32_t n_quant, int32_t n_res);
+int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q, int64_t q_stride, const void* k_new,
+                             const void* v_new, int64_t kv_stride, kvq_chunk chunk, kvq_qcache qcache, kvq_residual res,
+                             const int32_t* seq_state, int32_t n_quant, int32_t res_start, int32_t n_res,
+                             kvq_pool pool, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Take a chunk up into a cache that may hold tokens already: the state that appending its tokens one by one would leave
+ * (kvq_append_residual, and where a ring fills kvq_trace_outliers and kvq_quantize_group), bit for bit but for ring rows
+ * that hold no token afterwards, which may differ.  A sequence with n_res ring rows and n new tokens has
+ * floor((n_res + n - R) / G) groups traced and quantized, in order (none if n_res + n < R + G).
+ *   k_new, v_new, kv_stride, chunk : as in kvq_prompt_attention (not NULL)
+ *   seq_state  : device state of every sequence (read only: call this for every layer with the same array, then
+ *                kvq_seq_extend once); n_quant, res_start, n_res are ignored.  A sequence that is inactive, whose state
+ *                is not one that these calls produce, or whose groups do not fit max_seq, is left alone by both calls.
+ *                NULL: the three numbers are every sequence's state, n_res < R + G, res_start a multiple of group_k, and the
+ *                groups have to fit (KVQ_ERR_INVALID_ARG); the caller then counts on for itself: n_quant + groups * G,
+ *                (res_start + groups * G) mod res_rows, n_res + n - groups * G
+ *   selected   : device uint8 scratch of at least batch * kv_heads * G * ((max_tokens + G - 1) / G) bytes
+ *                (KVQ_ERR_WORKSPACE below), contents unspecified on return
+ *   qcache     : dense or paged; the table's entries of the new groups must be in place
+ * KVQ_ERR_UNSUPPORTED with value_per_step.
+ *
+ * kvq_seq_extend applies the chunk to the array of states: the same rule for n tokens that kvq_seq_advance has for one.
+ */
+int32_t kvq_extend(const kvq_config* cfg, int32_t layer, const void* k_new, const void* v_new, int64_t kv_stride,
+                   kvq_chunk chunk, kvq_residual res, const int32_t* seq_state, int32_t n_quant, int32_t res_start,
+                   int32_t n_res, kvq_pool pool, uint8_t* selected, size_t selected_bytes, kvq_qcache qcache, void* stream);
+int32_t kvq_seq_extend(const kvq_config* cfg, int32_t* seq_state, kvq_chunk chunk, void* stream);
+
+/*
+ * Sequences that take over others (requests behind one system prompt, beams): for every pair {from, to} of `pairs`,
+ * sequence `to` becomes what sequence `from` was before the call, in every layer, all pairs at once (a sequence may
+ * be the source of many and the target of one, of itself too, and chains and rings of them are fine).
+ *   pairs      : device int32 [n_pairs][2], 4-byte aligned, 1 <= n_pairs <= batch.  A pair with a number outside
+ *                [0, batch) is skipped.  Two pairs must not name the same target (its contents are unspecified then)
+ *   seq_state  : the array of states, whose entries are copied too; or NULL: n_quant, res_start, n_res are the state of
+ *                every sequence
+ *   copied     : live ring rows, members of both pools with index and score, counts and frozen flags.  What holds no
+ *                token is left as it was in the target
+ *   page_table : for a paged cache qcache.page_table again, as memory to write to (KVQ_ERR_INVALID_ARG if it is another;
+ *                NULL for a dense cache).  The entries of the source's quantized groups are copied: the sequences share
+ *                those pages from then on.  That is safe, for a page is written once, when its group is quantized, and only
+ *                read afterwards; entries of later groups stay the target's own.  Before a sequence that shares pages
+ *                starts anew (kvq_prefill_quantize_seq, kvq_prefill_sequence), its table row must name other pages
+ *                In a dense cache the groups themselves are copied
+ *   n_pairs above 1024: KVQ_ERR_UNSUPPORTED
+ */
+int32_t kvq_fork_sequences(const kvq_config* cfg, const int32_t* pairs, int32_t n_pairs, int32_t* seq_state, int32_t n_quant,
+                           int32_t res_start, int32_t n_res, kvq_residual res, kvq_pool pool, kvq_qcache qcache,
+                           int32_t* page_table, void* stream);
+
+/*
+ * Pages of a paged cache.  A page is live if a table entry of a quantized group names it (groups j < n_quant / G of each
+ * sequence, with n_quant from seq_state, or, where that is NULL, the argument for every sequence; entries that name no page of
+ * the pool count for nothing).  Several entries may name one page (kvq_fork_sequences).
+ *
+ * kvq_free_pages : lists the pages that are not live.
+ *   free_pages : device int32 [n_pages], out: their numbers, ascending, then -1 in the entries that are left
+ *   counts     : device int32 [2], out: {free pages, live pages}
+ *
+ * kvq_copy_pages : page pairs[i][0] of `from` becomes page pairs[i][1] of `to`, every layer and kv head, codes, steps,
+ *                zeros and masks.  Both have the same configuration but for n_pages; their tables are not read and may be NULL.
+ *   pairs      : device int32 [n_pairs][2], 4-byte aligned; a pair with a number outside its pool is skipped.  No page may be
+ *                the target of two pairs, nor, where `from` and `to` are one pool, a target and a source
+ *
+ * kvq_compact_pages : the live pages of `from`, ascending, become pages 0, 1, ... of the pool `to`, which must not share
+ *                memory with `from`: a pool that has to grow or shrink, or that is to be handed on in one piece.  Shared pages stay
+ *                shared.
+ *   to         : its arrays and n_pages (to.page_table is not read).  Live pages that find no room are left out
+ *   to_table   : device int32 [batch][to.table_stride], out, 4-byte aligned: of live groups the new page, of all other entries
+ *                -1.  A group whose page found no room gets -1, too
+ *   counts     : device int32 [2], out: {free pages of `from`, live pages}: all have found room if counts[1] <= to.n_pages
+ *   workspace  : device int32, at least from.n_pages entries (KVQ_ERR_WORKSPACE below), 4-byte aligned
+ */
+int32_t kvq_free_pages(const kvq_config* cfg, kvq_qcache qcache, const int32_t* seq_state, int32_t n_quant,
+                       int32_t* free_pages, int32_t* counts, void* stream);
+int32_t kvq_copy_pages(const kvq_config* cfg, kvq_qcache from, kvq_qcache to, const int32_t* pairs, int32_t n_pairs,
+                       void* stream);
+int32_t kvq_compact_pages(const kvq_config* cfg, kvq_qcache from, const int32_t* seq_state, int32_t n_quant, kvq_qcache to,
+                          int32_t* to_table, int32_t* counts, int32_t* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The rotary position embedding of kvq_append_decode_attention_rope for positions with several axes (text: one; images:
+ * height and width; video: time as well): channel pair i of a token turns by positions[pair_axis[i]][token] * freq[i].
+ * The product is taken in fp64 and reduced to one turn before the cosine and the sine, which are fp32; the rotation itself
+ * is rounded as there (each product and the sum to fp32, the result to fp16), so rotating with kvq_rope_rows' rows
+ * (kvq_rope_rotate, kvq_append_decode_attention_rope) gives the same bits.
+ *   positions  : device int32 [axes][tokens], 4-byte aligned; any value
+ *   axes       : 1 .. 8
+ *   pair_axis  : HOST uint8 [head_dim / 2], each below axes (it may go when the call returns)
+ *   freq       : device fp32 [head_dim / 2], 4-byte aligned: radians per position, finite
+ *   tokens     : 1 .. 2^31 - 1
+ *
+ * kvq_rope_axes : rows of `tokens` tokens: their q_heads query rows and their kv_heads Key rows.
+ *   q, k       : device fp16, 16-byte aligned, token i at element offset i * q_stride (k_stride); strides as in
+ *                kvq_prompt_attention.  One of them may be NULL (with its output)
+ *   q_out, k_out : device fp16, 16-byte aligned, with strides of their own; q_out may be q and k_out may be k with the same stride,
+ *                otherwise outputs must not overlap inputs
+ * kvq_rope_rows : the rows themselves, for a decode step.
+ *   rows       : device fp32 [tokens][head_dim], out, 16-byte aligned: head_dim / 2 cosines, then the sines: what
+ *                kvq_append_decode_attention_rope takes with rope_stride = head_dim
+ */
+int32_t kvq_rope_axes(const kvq_config* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                      int32_t tokens, const int32_t* positions, int32_t axes, const uint8_t* pair_axis, const float* freq,
+                      void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream);
+int32_t kvq_rope_rows(const kvq_config* cfg, int32_t tokens, const int32_t* positions, int32_t axes,
+                      const uint8_t* pair_axis, const float* freq, float* rows, void* stream);
+
+/*
  * The quantized segment as fp16 rows, for consumers that need the cache as a matrix (attention of
  * several query tokens at once, inspection): x^ = X_min + Q * q, the inverse of Eq. 2, evaluated in
  * fp32 (the product is exact there, the sum rounds once) and rounded to nearest fp16.  A token that
@@ -550,7 +708,7 @@ int32_t kvq_stream_read(const void* buf, size_t bytes, void* sink, void* stream)
 /* Static string for a kvq_status value. */
 const char* kvq_status_string(int32_t status);
 
-/* Version of this interface (structure layouts and entry points), for the binding's load check: 6. */
+/* Version of this interface (structure layouts and entry points), for the binding's load check: 8. */
 int32_t kvq_version(void);
 
 #ifdef __cplusplus

@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(HERE, "libkvq.so")
 
 KVQ_OK, KVQ_ERR_INVALID_ARG, KVQ_ERR_UNSUPPORTED, KVQ_ERR_WORKSPACE, KVQ_ERR_LAUNCH, KVQ_ERR_SCRATCH = 0, -1, -2, -3, -4, -5
 
-INTERFACE_VERSION = 7       # kvq_version() of the library these structures and signatures match
+INTERFACE_VERSION = 8       # kvq_version() of the library these structures and signatures match
 EXPORTS = ["kvq_query_sizes", "kvq_append_residual", "kvq_trace_outliers", "kvq_quantize_group",
            "kvq_append_trace_quantize", "kvq_prefill_quantize", "kvq_prefill_quantize_seq", "kvq_prefill_sequence",
            "kvq_decode_attention",
@@ -25,6 +25,8 @@ EXPORTS = ["kvq_query_sizes", "kvq_append_residual", "kvq_trace_outliers", "kvq_
            "kvq_decode_attention_ragged", "kvq_decode_attention_multi", "kvq_decode_workspace_bytes",
            "kvq_decode_launch_shape", "kvq_decode_attention_static", "kvq_dequantize", "kvq_stream_read",
            "kvq_quantize_value_tokens", "kvq_seq_plan_bytes", "kvq_seq_plan", "kvq_decode_attention_planned",
+           "kvq_prompt_workspace_bytes", "kvq_prompt_attention", "kvq_extend", "kvq_seq_extend", "kvq_fork_sequences",
+           "kvq_free_pages", "kvq_copy_pages", "kvq_compact_pages", "kvq_rope_axes", "kvq_rope_rows",
            "kvq_status_string", "kvq_version"]
 
 
@@ -54,6 +56,10 @@ class kvq_pool(C.Structure):
 
 class kvq_residual(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k_res", "v_res")]
+
+
+class kvq_chunk(C.Structure):
+    _fields_ = [("starts", C.c_void_p), ("total", C.c_int32), ("max_tokens", C.c_int32)]
 
 
 class KvqError(RuntimeError):
@@ -138,6 +144,28 @@ def load_library() -> C.CDLL:
     lib.kvq_decode_attention_planned.restype = i32
     lib.kvq_decode_attention_planned.argtypes = [cfgp, i32, vp, kvq_qcache, kvq_residual, vp, i32, i32, kvq_pool,
                                                  vp, vp, C.c_size_t, vp]
+    lib.kvq_prompt_workspace_bytes.restype = i64
+    lib.kvq_prompt_workspace_bytes.argtypes = [cfgp, i32, i32, i32]
+    lib.kvq_prompt_attention.restype = i32
+    lib.kvq_prompt_attention.argtypes = [cfgp, i32, vp, i64, vp, vp, i64, kvq_chunk, kvq_qcache, kvq_residual, vp, i32, i32,
+                                         i32, kvq_pool, vp, vp, C.c_size_t, vp]
+    lib.kvq_extend.restype = i32
+    lib.kvq_extend.argtypes = [cfgp, i32, vp, vp, i64, kvq_chunk, kvq_residual, vp, i32, i32, i32, kvq_pool, vp, C.c_size_t,
+                               kvq_qcache, vp]
+    lib.kvq_seq_extend.restype = i32
+    lib.kvq_seq_extend.argtypes = [cfgp, vp, kvq_chunk, vp]
+    lib.kvq_fork_sequences.restype = i32
+    lib.kvq_fork_sequences.argtypes = [cfgp, vp, i32, vp, i32, i32, i32, kvq_residual, kvq_pool, kvq_qcache, vp, vp]
+    lib.kvq_free_pages.restype = i32
+    lib.kvq_free_pages.argtypes = [cfgp, kvq_qcache, vp, i32, vp, vp, vp]
+    lib.kvq_copy_pages.restype = i32
+    lib.kvq_copy_pages.argtypes = [cfgp, kvq_qcache, kvq_qcache, vp, i32, vp]
+    lib.kvq_compact_pages.restype = i32
+    lib.kvq_compact_pages.argtypes = [cfgp, kvq_qcache, vp, i32, kvq_qcache, vp, vp, vp, C.c_size_t, vp]
+    lib.kvq_rope_axes.restype = i32
+    lib.kvq_rope_axes.argtypes = [cfgp, vp, i64, vp, i64, i32, vp, i32, C.c_char_p, vp, vp, i64, vp, i64, vp]
+    lib.kvq_rope_rows.restype = i32
+    lib.kvq_rope_rows.argtypes = [cfgp, i32, vp, i32, C.c_char_p, vp, vp, vp]
     _lib = lib
     return lib
 
@@ -361,6 +389,95 @@ def kvq_decode_attention_planned(cfg, layer, q, qcache: kvq_qcache, res: kvq_res
                                                      workspace_bytes, _stream(stream))
     if st != KVQ_OK:
         raise KvqError(st, "kvq_decode_attention_planned")
+
+
+def kvq_prompt_workspace_bytes(cfg, max_tokens, n_quant, n_res) -> int:
+    n = load_library().kvq_prompt_workspace_bytes(C.byref(cfg), max_tokens, n_quant, n_res)
+    if n < 0:
+        raise KvqError(int(n), "kvq_prompt_workspace_bytes")
+    return int(n)
+
+
+def kvq_prompt_attention(cfg, layer, q, q_stride, k_new, v_new, kv_stride, chunk: kvq_chunk, qcache: kvq_qcache,
+                         res: kvq_residual, seq_state, n_quant, res_start, n_res, pool: kvq_pool, out, workspace,
+                         workspace_bytes, stream=None):
+    st = load_library().kvq_prompt_attention(C.byref(cfg), layer, _ptr(q), q_stride, _ptr(k_new), _ptr(v_new), kv_stride,
+                                             chunk, qcache, res, _ptr(seq_state), n_quant, res_start, n_res, pool,
+                                             _ptr(out), _ptr(workspace), workspace_bytes, _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_prompt_attention")
+
+
+def kvq_extend(cfg, layer, k_new, v_new, kv_stride, chunk: kvq_chunk, res: kvq_residual, seq_state, n_quant, res_start,
+               n_res, pool: kvq_pool, selected, selected_bytes, qcache: kvq_qcache, stream=None):
+    st = load_library().kvq_extend(C.byref(cfg), layer, _ptr(k_new), _ptr(v_new), kv_stride, chunk, res, _ptr(seq_state),
+                                   n_quant, res_start, n_res, pool, _ptr(selected), selected_bytes, qcache,
+                                   _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_extend")
+
+
+def kvq_seq_extend(cfg, seq_state, chunk: kvq_chunk, stream=None):
+    st = load_library().kvq_seq_extend(C.byref(cfg), _ptr(seq_state), chunk, _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_seq_extend")
+
+
+def kvq_fork_sequences(cfg, pairs, n_pairs, seq_state, n_quant, res_start, n_res, res: kvq_residual, pool: kvq_pool,
+                       qcache: kvq_qcache, page_table, stream=None):
+    st = load_library().kvq_fork_sequences(C.byref(cfg), _ptr(pairs), n_pairs, _ptr(seq_state), n_quant, res_start, n_res,
+                                           res, pool, qcache, _ptr(page_table), _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_fork_sequences")
+
+
+def kvq_free_pages(cfg, qcache: kvq_qcache, seq_state, n_quant, free_pages, counts, stream=None):
+    st = load_library().kvq_free_pages(C.byref(cfg), qcache, _ptr(seq_state), n_quant, _ptr(free_pages), _ptr(counts),
+                                       _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_free_pages")
+
+
+def kvq_copy_pages(cfg, source: kvq_qcache, to: kvq_qcache, pairs, n_pairs, stream=None):
+    st = load_library().kvq_copy_pages(C.byref(cfg), source, to, _ptr(pairs), n_pairs, _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_copy_pages")
+
+
+def kvq_compact_pages(cfg, source: kvq_qcache, seq_state, n_quant, to: kvq_qcache, to_table, counts, workspace,
+                      workspace_bytes, stream=None):
+    st = load_library().kvq_compact_pages(C.byref(cfg), source, _ptr(seq_state), n_quant, to, _ptr(to_table),
+                                          _ptr(counts), _ptr(workspace), workspace_bytes, _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_compact_pages")
+
+
+def _axes(cfg, pair_axis):
+    """The axis of every channel pair as the bytes that the library reads (None: all of them turn by the first)."""
+    pairs = cfg.head_dim // 2
+    if pair_axis is None:
+        return bytes(pairs)
+    if len(pair_axis) != pairs or not all(0 <= int(a) < 256 for a in pair_axis):
+        raise KvqError(KVQ_ERR_INVALID_ARG, "pair_axis")
+    return bytes(int(a) for a in pair_axis)
+
+
+def kvq_rope_axes(cfg, q, q_stride, k, k_stride, tokens, positions, axes, pair_axis, freq, q_out, q_out_stride, k_out,
+                  k_out_stride, stream=None):
+    """pair_axis: a sequence of head_dim / 2 numbers, or None (one axis)."""
+    st = load_library().kvq_rope_axes(C.byref(cfg), _ptr(q), q_stride, _ptr(k), k_stride, tokens, _ptr(positions), axes,
+                                      _axes(cfg, pair_axis), _ptr(freq), _ptr(q_out), q_out_stride, _ptr(k_out),
+                                      k_out_stride, _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_rope_axes")
+
+
+def kvq_rope_rows(cfg, tokens, positions, axes, pair_axis, freq, rows, stream=None):
+    """pair_axis: as in kvq_rope_axes."""
+    st = load_library().kvq_rope_rows(C.byref(cfg), tokens, _ptr(positions), axes, _axes(cfg, pair_axis), _ptr(freq),
+                                      _ptr(rows), _stream(stream))
+    if st != KVQ_OK:
+        raise KvqError(st, "kvq_rope_rows")
 
 
 def kvq_stream_read(buf, nbytes, sink, stream=None):

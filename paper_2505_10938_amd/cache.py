@@ -32,6 +32,33 @@ def _on(stream, device):
     return torch.cuda.stream(stream)
 
 
+def _token_rows(t, heads, head_dim):
+    """A packed array of tokens, [..., heads, head_dim] fp16 with rows of a token behind each other, as (tensor, tokens,
+    elements from token to token)."""
+    if t.dtype != torch.float16 or t.dim() < 3 or tuple(t.shape[-2:]) != (heads, head_dim):
+        raise ValueError(f"fp16 [..., {heads}, {head_dim}] is wanted, not {t.dtype} {tuple(t.shape)}")
+    rows = t.view(-1, heads, head_dim)                     # (a RuntimeError if the tokens are not evenly spaced)
+    if rows.shape[0] == 0 or (heads > 1 and rows.stride(1) != head_dim) or rows.stride(2) != 1:
+        raise ValueError("a token's heads have to lie behind each other, and there has to be one token at least")
+    return rows, rows.shape[0], rows.stride(0) if rows.shape[0] > 1 else heads * head_dim
+
+
+class PagePool:
+    """The quantized arrays of a paged cache: `n_pages` pages of one Key group each, for all layers and kv heads, and a
+    table [batch, max_seq / G] that names them (-1: none)."""
+
+    def __init__(self, cfg: B.kvq_config, n_pages, device="cuda:0"):
+        self.cfg, self.n_pages, self.device = cfg, n_pages, torch.device(device)
+        sz = B.kvq_query_sizes(make_config(cfg.layers, 1, cfg.kv_heads, cfg.kv_heads, n_pages * cfg.group_k, cfg.bits,
+                                           cfg.group_k, cfg.group_v, cfg.residual, cfg.outlier_budget, cfg.aux_capacity,
+                                           cfg.head_dim, 0, cfg.value_per_step))
+        for name in ("k_codes", "k_meta", "v_codes", "v_meta", "mask"):
+            setattr(self, name, torch.zeros(getattr(sz, name + "_bytes"), dtype=torch.uint8, device=self.device))
+        self.page_table = torch.full((cfg.batch, cfg.max_seq // cfg.group_k), -1, dtype=torch.int32, device=self.device)
+        self.qcache = B.kvq_qcache(*(t.data_ptr() for t in (self.k_codes, self.k_meta, self.v_codes, self.v_meta, self.mask,
+                                                            self.page_table)), self.page_table.shape[1], n_pages)
+
+
 class KVCache:
     """All caller-owned buffers of kvq for one configuration, on one device.
 
@@ -265,6 +292,196 @@ class KVCache:
         self.n_res[layer] += 1
         return out
 
+    # ---- chunks of tokens ------------------------------------------------------------------------------
+    def _behind_prompts(self, stream):
+        pass
+
+    def _launching(self, stream):
+        """Context in which a call's tensors belong to `stream` (None: the current one) of the cache's device."""
+        if stream is not None:
+            return _on(stream, self.device)
+        return torch.cuda.device(self.device) if self.device.type == "cuda" else contextlib.nullcontext()
+
+    def _attend(self, layer, q, k_new, v_new, starts, max_tokens, seq_state, state, out, stream):
+        cfg = self.cfg
+        rows, total, q_stride = _token_rows(q, cfg.q_heads, cfg.head_dim)
+        kv_stride = 0
+        if (k_new is None) != (v_new is None):
+            raise ValueError("new Keys and new Values come together")
+        if k_new is not None:
+            (k_new, nk, kv_stride), (v_new, nv, v_stride) = (_token_rows(t, cfg.kv_heads, cfg.head_dim) for t in (k_new, v_new))
+            if nk != total or nv != total or v_stride != kv_stride:
+                raise ValueError("queries, new Keys and new Values are of the same tokens, Keys and Values equally spaced")
+        self._behind_prompts(stream)
+        with self._launching(stream):
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+                raise ValueError("the output is fp16, contiguous, of the queries' shape")
+            n_quant, res_start, n_res = state
+            need = B.kvq_prompt_workspace_bytes(cfg, max_tokens, n_quant, n_res)
+            # (of this call's own: calls on two streams, or in two captured graphs, do not meet in it)
+            workspace = torch.empty(need, dtype=torch.uint8, device=self.device) if need else None
+            B.kvq_prompt_attention(cfg, layer, rows, q_stride, k_new, v_new, kv_stride,
+                                   B.kvq_chunk(None if starts is None else starts.data_ptr(), total, max_tokens),
+                                   self.qcache, self.res, seq_state, n_quant, res_start, n_res, self.pool, out, workspace,
+                                   need, stream)
+        return out
+
+    def attend(self, layer, q, k_new=None, v_new=None, out=None, stream=None):
+        """Attention of a chunk of new tokens (q: fp16 [batch, tokens, q_heads, head_dim]; k_new, v_new: fp16 [batch,
+        tokens, kv_heads, head_dim]; tokens evenly spaced) over the cache and, causally, the chunk itself.  Without k_new
+        and v_new every query sees the whole cache and nothing else.  The cache is not changed: see extend()."""
+        return self._attend(layer, q, k_new, v_new, None, q.shape[1], None,
+                            (self.n_quant[layer], self.res_start[layer], self.n_res[layer]), out, stream)
+
+    def _extend(self, layer, k_new, v_new, starts, max_tokens, seq_state, state, stream):
+        cfg = self.cfg
+        (k_rows, total, stride), (v_rows, nv, v_stride) = (_token_rows(t, cfg.kv_heads, cfg.head_dim) for t in (k_new, v_new))
+        if nv != total or v_stride != stride:
+            raise ValueError("new Keys and new Values are of the same tokens, equally spaced")
+        self._behind_prompts(stream)
+        G = cfg.group_k
+        with self._launching(stream):
+            selected = torch.empty(cfg.batch * cfg.kv_heads * G * ((max_tokens + G - 1) // G), dtype=torch.uint8,
+                                   device=self.device)
+            B.kvq_extend(cfg, layer, k_rows, v_rows, stride,
+                         B.kvq_chunk(None if starts is None else starts.data_ptr(), total, max_tokens), self.res, seq_state,
+                         *state, self.pool, selected, selected.numel(), self.qcache, stream)
+
+    def extend(self, layer, k_new, v_new, stream=None):
+        """A chunk of tokens (as in attend()) joins the cache of `layer`: the state that appending them one by one would
+        leave."""
+        cfg, n = self.cfg, k_new.shape[1]
+        G, R = cfg.group_k, cfg.residual
+        state = (self.n_quant[layer], self.res_start[layer], self.n_res[layer])
+        self._extend(layer, k_new, v_new, None, n, None, state, stream)
+        n += self.n_res[layer]
+        done = G * ((n - R) // G) if n >= R + G else 0
+        self.n_quant[layer] += done
+        self.res_start[layer] = (self.res_start[layer] + done) % self.sizes.res_rows
+        self.n_res[layer] = n - done
+
+    def rotate(self, q, k, positions, freq, pair_axis=None, q_out=None, k_out=None, stream=None):
+        """The rotary position embedding of a chunk's queries (fp16 [..., q_heads, head_dim], tokens evenly spaced) and
+        Keys (fp16 [..., kv_heads, head_dim]; either may be None) at `positions` (int32 [axes, tokens] or [tokens]):
+        channel pair i turns by positions[pair_axis[i]] * freq[i] (fp32 [head_dim / 2]; pair_axis: head_dim / 2 numbers, None:
+        all 0).  Returns the rotated queries and Keys; outputs may be the inputs themselves."""
+        cfg = self.cfg
+        positions, axes, tokens = self._positions(positions, freq)
+        outs, args = [], []
+        with self._launching(stream):
+            for x, out, heads in ((q, q_out, cfg.q_heads), (k, k_out, cfg.kv_heads)):
+                if x is None:
+                    outs.append(None)
+                    args.append((None, 0, None, 0))
+                    continue
+                if out is None:
+                    out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+                (rows, n, stride), (to, m, to_stride) = (_token_rows(t, heads, cfg.head_dim) for t in (x, out))
+                if n != tokens or m != tokens:
+                    raise ValueError("there has to be a position for every token, and an output")
+                outs.append(out)
+                args.append((rows, stride, to, to_stride))
+            (q, qs, qo, qos), (k, ks, ko, kos) = args
+            B.kvq_rope_axes(cfg, q, qs, k, ks, tokens, positions, axes, pair_axis, freq, qo, qos, ko, kos, stream)
+        return tuple(outs)
+
+    def rope_rows(self, positions, freq, pair_axis=None, out=None, stream=None):
+        """The cosines and sines that step(..., rope=, rope_stride=head_dim) takes, one row (fp32 [tokens, head_dim]) for
+        each position; arguments as in rotate()."""
+        cfg = self.cfg
+        positions, axes, tokens = self._positions(positions, freq)
+        with self._launching(stream):
+            if out is None:
+                out = torch.empty(tokens, cfg.head_dim, dtype=torch.float32, device=positions.device)
+            elif out.shape != (tokens, cfg.head_dim) or out.dtype != torch.float32 or not out.is_contiguous():
+                raise ValueError("the rows are fp32 [tokens, head_dim], contiguous")
+            B.kvq_rope_rows(cfg, tokens, positions, axes, pair_axis, freq, out, stream)
+        return out
+
+    def _positions(self, positions, freq):
+        if positions.dtype != torch.int32 or positions.dim() not in (1, 2) or not positions.is_contiguous():
+            raise ValueError("positions are int32 [axes, tokens], contiguous")
+        if freq.dtype != torch.float32 or freq.shape != (self.cfg.head_dim // 2,) or not freq.is_contiguous():
+            raise ValueError("frequencies are fp32 [head_dim / 2], contiguous")
+        return positions, 1 if positions.dim() == 1 else positions.shape[0], positions.shape[-1]
+
+    # ---- sequences and pages ---------------------------------------------------------------------------
+    def _sequences(self):
+        """(array of states or None, the state of every sequence) for calls that concern all layers."""
+        states = set(zip(self.n_quant, self.res_start, self.n_res))
+        if len(states) != 1:
+            raise ValueError("the layers are not at the same token")
+        return None, states.pop()
+
+    def fork(self, pairs, stream=None):
+        """For every row {from, to} of `pairs` (int32 [n, 2], device), sequence `to` becomes what sequence `from` was before
+        the call, in all layers.  In a paged cache the two share the pages of whole groups."""
+        self._pairs(pairs)
+        if pairs.shape[0] == 0:
+            return
+        self._behind_prompts(stream)
+        seq_state, state = self._sequences()
+        with self._launching(stream):
+            B.kvq_fork_sequences(self.cfg, pairs, pairs.shape[0], seq_state, *state, self.res, self.pool, self.qcache,
+                                 self.page_table, stream)
+
+    def _pairs(self, pairs):
+        if pairs.dtype != torch.int32 or pairs.dim() != 2 or pairs.shape[1] != 2 or not pairs.is_contiguous():
+            raise ValueError("pairs are int32 [n, 2], contiguous")
+
+    def _paged(self):
+        if self.page_table is None:
+            raise ValueError("the cache has no pages")
+
+    def free_pages(self, stream=None):
+        """The pages that no quantized group of any sequence lies in: (int32 [n_pages], ascending, then -1; int32 [2]: free
+        pages, live pages), both on the device."""
+        self._paged()
+        self._behind_prompts(stream)
+        seq_state, state = self._sequences()
+        with self._launching(stream):
+            free = torch.empty(self.n_pages, dtype=torch.int32, device=self.device)
+            counts = torch.empty(2, dtype=torch.int32, device=self.device)
+            B.kvq_free_pages(self.cfg, self.qcache, seq_state, state[0], free, counts, stream)
+        return free, counts
+
+    def copy_pages(self, pairs, to=None, stream=None):
+        """For every row {from, to} of `pairs` (int32 [n, 2], device), a page becomes a page of the pool `to` (a PagePool;
+        None: of the same pool)."""
+        self._paged()
+        self._pairs(pairs)
+        if pairs.shape[0] == 0:
+            return
+        self._behind_prompts(stream)
+        with self._launching(stream):
+            B.kvq_copy_pages(self.cfg, self.qcache, self.qcache if to is None else to.qcache, pairs, pairs.shape[0], stream)
+
+    def compact_into(self, to, stream=None):
+        """The live pages, ascending, become pages 0, 1, ... of the PagePool `to`, with its table.  Returns int32 [2] on the
+        device: free and live pages (if there are more of these than `to` has pages, some were left out).  adopt(to) then
+        makes it the cache's own."""
+        self._paged()
+        if to.k_codes.data_ptr() == self.k_codes.data_ptr():
+            raise ValueError("a pool is not compacted into itself")
+        self._behind_prompts(stream)
+        seq_state, state = self._sequences()
+        with self._launching(stream):
+            counts = torch.empty(2, dtype=torch.int32, device=self.device)
+            work = torch.empty(self.n_pages, dtype=torch.int32, device=self.device)
+            B.kvq_compact_pages(self.cfg, self.qcache, seq_state, state[0], to.qcache, to.page_table, counts, work,
+                                4 * self.n_pages, stream)
+        return counts
+
+    def adopt(self, pool):
+        """The arrays and the table of a PagePool become the cache's (those that it had are given back with the last
+        reference to them: calls that still use them have to be on the current stream, or through)."""
+        self._paged()
+        for name in ("k_codes", "k_meta", "v_codes", "v_meta", "mask", "page_table", "n_pages"):
+            setattr(self, name, getattr(pool, name))
+        self._bind()
+
     def clone(self):
         """A second cache with the same contents in its own device memory."""
         other = KVCache.__new__(KVCache)
@@ -397,6 +614,37 @@ class RaggedKVCache(KVCache):
             cfg, b, k_rows, v_rows, n * cfg.head_dim, n, self.pool, self.prefill_selected, self.prefill_selected.numel(),
             self.qcache, self.res, self.seq_state, bool(active), at))
         self.longest = max(self.longest, n)
+
+    def attend(self, layer, q, starts, max_tokens, k_new=None, v_new=None, out=None, stream=None):
+        """Attention of new tokens over their sequences' caches and, causally, over themselves: q fp16 [total, q_heads,
+        head_dim], k_new and v_new fp16 [total, kv_heads, head_dim] (tokens evenly spaced); sequence b's are rows starts[b]
+        .. starts[b + 1] - 1 (int32 [batch + 1], device), `max_tokens` of them at most.  Without k_new and v_new every query
+        sees its sequence's whole cache and nothing else.  Rows of no sequence are left as they are (a new output's hold
+        anything)."""
+        self._starts(starts)
+        nq, nr = self.bounds()
+        return self._attend(layer, q, k_new, v_new, starts, max_tokens, self.seq_state, (nq, 0, nr), out, stream)
+
+    def extend(self, layer, k_new, v_new, starts, max_tokens, stream=None):
+        """New tokens (as in attend()) join `layer` of their sequences' caches, where these are active: the state that
+        appending them one by one would leave.  Call for every layer, then advance_by()."""
+        self._starts(starts)
+        self._extend(layer, k_new, v_new, starts, max_tokens, self.seq_state, (0, 0, 0), stream)
+
+    def advance_by(self, starts, max_tokens, stream=None):
+        """The sequences' states after the tokens that extend() has put into every layer."""
+        self._starts(starts)
+        self._behind_prompts(stream)
+        with self._launching(stream):
+            B.kvq_seq_extend(self.cfg, self.seq_state, B.kvq_chunk(starts.data_ptr(), 2 ** 31 - 1, max_tokens), stream)
+        self.longest += max_tokens
+
+    def _starts(self, starts):
+        if starts.dtype != torch.int32 or starts.shape != (self.cfg.batch + 1,) or not starts.is_contiguous():
+            raise ValueError("starts are int32 [batch + 1], contiguous")
+
+    def _sequences(self):
+        return self.seq_state, (self.bounds()[0], 0, 0)
 
     def advance(self, stream=None):
         """The sequences' states after the token just appended to every layer."""

@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(256) stream_read_kernel(const uint4* __restric
 
 extern "C" {
 
-int32_t kvq_version(void) { return 7; }
+int32_t kvq_version(void) { return 8; }
 
 int32_t kvq_stream_read(const void* buf, size_t bytes, void* sink, void* stream) {
   if (!buf || !sink || bytes == 0 || bytes % 16 != 0 || ((uintptr_t)buf & 15) != 0) return KVQ_ERR_INVALID_ARG;
@@ -830,6 +830,301 @@ int32_t kvq_decode_attention_ragged(const kvq_config* cfg, int32_t layer, const 
   if (!seq_state || (((uintptr_t)seq_state) & 15)) return KVQ_ERR_INVALID_ARG;
   return decode_common(cfg, layer, q, 1, qc, max_n_quant, res, 0, max_n_res, seq_state, nullptr, nullptr, pool, out,
                        workspace, workspace_bytes, stream);
+}
+
+namespace {
+
+int32_t shift_of(int32_t power) { return power == 1 ? 0 : power == 2 ? 1 : power == 4 ? 2 : 3; }
+
+// The chunk's rows as the kernels take them, and where they are: token i of a packed array at element offset i * stride.
+int32_t check_chunk(const kvq_config* cfg, const kvq_chunk& c) {
+  if (c.total < 1 || c.max_tokens < 1 || c.max_tokens > c.total) return KVQ_ERR_INVALID_ARG;
+  if (((uintptr_t)c.starts) & 3) return KVQ_ERR_INVALID_ARG;
+  if (!c.starts && (int64_t)cfg->batch * c.max_tokens != c.total) return KVQ_ERR_INVALID_ARG;
+  return KVQ_OK;
+}
+bool rows_ok(const void* p, int64_t stride, int64_t heads, int64_t head_dim) {
+  return p && (((uintptr_t)p) & 15) == 0 && stride >= heads * head_dim && stride % 8 == 0;
+}
+
+// How a chunk's attention is dealt: row tiles of a unit, and workgroups that share a row tile's keys where the row tiles
+// alone would not fill the device (two workgroups fit a compute unit); each then has at least two tiles of 64 keys.
+struct ChunkShape {
+  int64_t row_tiles, splits;
+};
+ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quant, int64_t n_res, bool with_new) {
+  const int64_t g = cfg->q_heads / cfg->kv_heads;
+  ChunkShape s;
+  s.row_tiles = (max_tokens * g + kvq::kChunkRows - 1) / kvq::kChunkRows;
+  const int64_t groups = (int64_t)cfg->batch * cfg->kv_heads * s.row_tiles;
+  const int64_t rows = n_res + cfg->outlier_budget + cfg->aux_capacity;
+  const int64_t tiles = (n_quant + 63) / 64 + (rows + 63) / 64 + (with_new ? (max_tokens + 63) / 64 : 0);
+  s.splits = 2 * kvq::kComputeUnits / groups;
+  if (s.splits > tiles / 2) s.splits = tiles / 2;
+  if (s.splits < 1) s.splits = 1;
+  return s;
+}
+int64_t chunk_workspace_bytes(const kvq_config* cfg, const ChunkShape& s) {
+  if (s.splits == 1) return 0;
+  return (int64_t)cfg->batch * cfg->kv_heads * s.row_tiles * kvq::kChunkRows * s.splits * (cfg->head_dim + 2) * 4;
+}
+
+}  // namespace
+
+int64_t kvq_prompt_workspace_bytes(const kvq_config* cfg, int32_t max_tokens, int32_t n_quant, int32_t n_res) {
+  const int32_t st = check_config(cfg);
+  if (st != KVQ_OK) return st;
+  if (max_tokens < 1 || n_quant < 0 || n_quant > cfg->max_seq || n_quant % cfg->group_k != 0) return KVQ_ERR_INVALID_ARG;
+  if (n_res < 0 || n_res > (int32_t)res_rows_of(cfg)) return KVQ_ERR_INVALID_ARG;
+  const int64_t with = chunk_workspace_bytes(cfg, chunk_shape(cfg, max_tokens, n_quant, n_res, true));
+  const int64_t without = chunk_workspace_bytes(cfg, chunk_shape(cfg, max_tokens, n_quant, n_res, false));
+  return with > without ? with : without;
+}
+
+int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q, int64_t q_stride, const void* k_new,
+                             const void* v_new, int64_t kv_stride, kvq_chunk chunk, kvq_qcache qc, kvq_residual res,
+                             const int32_t* seq_state, int32_t n_quant, int32_t res_start, int32_t n_res, kvq_pool pool,
+                             void* out, void* workspace, size_t workspace_bytes, void* stream) {
+  int32_t st = check_config(cfg);
+  if (st != KVQ_OK) return st;
+  if (layer < 0 || layer >= cfg->layers) return KVQ_ERR_INVALID_ARG;
+  st = check_chunk(cfg, chunk);
+  if (st != KVQ_OK) return st;
+  if (!rows_ok(q, q_stride, cfg->q_heads, cfg->head_dim)) return KVQ_ERR_INVALID_ARG;
+  if ((k_new != nullptr) != (v_new != nullptr)) return KVQ_ERR_INVALID_ARG;
+  if (k_new && (!rows_ok(k_new, kv_stride, cfg->kv_heads, cfg->head_dim) ||
+                !rows_ok(v_new, kv_stride, cfg->kv_heads, cfg->head_dim)))
+    return KVQ_ERR_INVALID_ARG;
+  if (!out || (((uintptr_t)out) & 7)) return KVQ_ERR_INVALID_ARG;
+  if (((uintptr_t)seq_state) & 15) return KVQ_ERR_INVALID_ARG;
+  if (n_quant < 0 || n_quant > cfg->max_seq || n_quant % cfg->group_k != 0) return KVQ_ERR_INVALID_ARG;
+  const int32_t rows = (int32_t)res_rows_of(cfg);
+  if (n_res < 0 || n_res > rows) return KVQ_ERR_INVALID_ARG;
+  if (!seq_state && (res_start < 0 || res_start >= rows)) return KVQ_ERR_INVALID_ARG;
+  if (!qcache_ok(cfg, qc) || !res.k_res || !res.v_res || !pool.pool_count || !pool.aux_count) return KVQ_ERR_INVALID_ARG;
+  if (cfg->outlier_budget + cfg->aux_capacity > 0 && (!pool.pool_k || !pool.pool_v)) return KVQ_ERR_INVALID_ARG;
+  if ((((uintptr_t)res.k_res) | ((uintptr_t)res.v_res) | ((uintptr_t)pool.pool_k) | ((uintptr_t)pool.pool_v) |
+       ((uintptr_t)qc.k_codes) | ((uintptr_t)qc.v_codes) | ((uintptr_t)qc.k_meta) | ((uintptr_t)qc.v_meta)) & 15)
+    return KVQ_ERR_INVALID_ARG;
+  if (((uintptr_t)qc.mask) & 3) return KVQ_ERR_INVALID_ARG;
+  const int64_t g = cfg->q_heads / cfg->kv_heads;
+  const ChunkShape shape = chunk_shape(cfg, chunk.max_tokens, n_quant, n_res, k_new != nullptr);
+  const int64_t items = (int64_t)cfg->batch * cfg->kv_heads * shape.row_tiles * shape.splits;
+  // (rows and the keys of a tile are numbered in 32 bits; a launch has less than 2^32 threads)
+  if (chunk.max_tokens * g > (1 << 30) || items > (1 << 24) - 16) return KVQ_ERR_UNSUPPORTED;
+  const int64_t need = chunk_workspace_bytes(cfg, shape);
+  if (need > 0 && (!workspace || (((uintptr_t)workspace) & 255) || (int64_t)workspace_bytes < need)) return KVQ_ERR_WORKSPACE;
+
+  kvq::ChunkArgs a;
+  a.d = make_dims(cfg, layer, qc);
+  a.q = (const __half*)q;
+  a.k_new = (const __half*)k_new;
+  a.v_new = (const __half*)v_new;
+  a.out = (__half*)out;
+  a.q_stride = q_stride;
+  a.kv_stride = kv_stride;
+  a.starts = chunk.starts;
+  a.total = chunk.total;
+  a.max_tokens = chunk.max_tokens;
+  a.k_codes = (const uint8_t*)qc.k_codes;
+  a.k_meta = (const uint8_t*)qc.k_meta;
+  a.v_codes = (const uint8_t*)qc.v_codes;
+  a.v_meta = (const uint8_t*)qc.v_meta;
+  a.mask = (const uint32_t*)qc.mask;
+  a.k_res = (const __half*)res.k_res;
+  a.v_res = (const __half*)res.v_res;
+  a.pool_k = (const __half*)pool.pool_k;
+  a.pool_v = (const __half*)pool.pool_v;
+  a.pool_count = pool.pool_count;
+  a.aux_count = pool.aux_count;
+  a.seq = seq_state;
+  a.n_quant = n_quant;
+  a.res_start = seq_state ? 0 : res_start;
+  a.n_res = n_res;
+  a.g_shift = shift_of((int32_t)g);
+  a.scale = 0.08838834764831845f * 1.4426950408889634f;
+  a.row_tiles = (int32_t)shape.row_tiles;
+  a.splits = (int32_t)shape.splits;
+  a.items = (uint32_t)items;
+  const int64_t shares = items * kvq::kChunkRows;
+  a.share_o = (float*)workspace;
+  a.share_ml = need > 0 ? a.share_o + shares * cfg->head_dim : nullptr;
+  return from_hip(kvq::launch_prompt_attention(a, (hipStream_t)stream));
+}
+
+int32_t kvq_extend(const kvq_config* cfg, int32_t layer, const void* k_new, const void* v_new, int64_t kv_stride,
+                   kvq_chunk chunk, kvq_residual res, const int32_t* seq_state, int32_t n_quant, int32_t res_start,
+                   int32_t n_res, kvq_pool pool, uint8_t* selected, size_t selected_bytes, kvq_qcache qc, void* stream) {
+  int32_t st = check_config(cfg);
+  if (st != KVQ_OK) return st;
+  if (layer < 0 || layer >= cfg->layers) return KVQ_ERR_INVALID_ARG;
+  if (cfg->value_per_step) return KVQ_ERR_UNSUPPORTED;
+  st = check_chunk(cfg, chunk);
+  if (st != KVQ_OK) return st;
+  if (!rows_ok(k_new, kv_stride, cfg->kv_heads, cfg->head_dim) || !rows_ok(v_new, kv_stride, cfg->kv_heads, cfg->head_dim))
+    return KVQ_ERR_INVALID_ARG;
+  if (!res.k_res || !res.v_res || ((((uintptr_t)res.k_res) | ((uintptr_t)res.v_res)) & 15)) return KVQ_ERR_INVALID_ARG;
+  if (((uintptr_t)seq_state) & 15) return KVQ_ERR_INVALID_ARG;
+  const int32_t G = cfg->group_k, R = cfg->residual;
+  if (!seq_state) {
+    if (n_quant < 0 || n_quant > cfg->max_seq || n_quant % G != 0) return KVQ_ERR_INVALID_ARG;
+    if (res_start < 0 || res_start >= (int32_t)res_rows_of(cfg) || res_start % G != 0) return KVQ_ERR_INVALID_ARG;
+    if (n_res < 0 || n_res >= R + G) return KVQ_ERR_INVALID_ARG;
+    // (with lengths on the device max_tokens is a bound only, and a sequence that does not fit is found there)
+    const int64_t held = (int64_t)n_res + chunk.max_tokens, groups = held >= R + G ? (held - R) / G : 0;
+    if (!chunk.starts && n_quant + groups * G > cfg->max_seq) return KVQ_ERR_INVALID_ARG;
+  }
+  if (!pool.pool_count || !pool.aux_count || !pool.frozen) return KVQ_ERR_INVALID_ARG;
+  if (cfg->outlier_budget > 0 && (!pool.pool_k || !pool.pool_v || !pool.pool_idx || !pool.pool_score))
+    return KVQ_ERR_INVALID_ARG;
+  if (!qcache_ok(cfg, qc) || !selected) return KVQ_ERR_INVALID_ARG;
+  const int64_t units = (int64_t)cfg->batch * cfg->kv_heads, most = ((int64_t)chunk.max_tokens + G - 1) / G;
+  if (chunk.max_tokens > (1 << 30) || units * most > (1 << 22) - 1) return KVQ_ERR_UNSUPPORTED;   // (threads of a launch)
+  if ((int64_t)selected_bytes < units * most * G) return KVQ_ERR_WORKSPACE;
+  return from_hip(kvq::launch_extend(make_dims(cfg, layer, qc), (const __half*)k_new, (const __half*)v_new, kv_stride, chunk,
+                                     res, seq_state, n_quant, res_start, n_res, pool, selected, qc, (hipStream_t)stream));
+}
+
+int32_t kvq_seq_extend(const kvq_config* cfg, int32_t* seq_state, kvq_chunk chunk, void* stream) {
+  int32_t st = check_config(cfg);
+  if (st != KVQ_OK) return st;
+  if (cfg->value_per_step) return KVQ_ERR_UNSUPPORTED;
+  if (!seq_state || (((uintptr_t)seq_state) & 15)) return KVQ_ERR_INVALID_ARG;
+  st = check_chunk(cfg, chunk);
+  if (st != KVQ_OK) return st;
+  return from_hip(kvq::launch_seq_extend(make_dims(cfg, 0), seq_state, chunk, (hipStream_t)stream));
+}
+
+int32_t kvq_fork_sequences(const kvq_config* cfg, const int32_t* pairs, int32_t n_pairs, int32_t* seq_state, int32_t n_quant,
+                           int32_t res_start, int32_t n_res, kvq_residual res, kvq_pool pool, kvq_qcache qc,
+                           int32_t* page_table, void* stream) {
+  const int32_t st = check_config(cfg);
+  if (st != KVQ_OK) return st;
+  if (!pairs || (((uintptr_t)pairs) & 3) || n_pairs < 1 || n_pairs > cfg->batch) return KVQ_ERR_INVALID_ARG;
+  if (((uintptr_t)seq_state) & 15) return KVQ_ERR_INVALID_ARG;
+  const int32_t rows = (int32_t)res_rows_of(cfg);
+  if (!seq_state && (n_quant < 0 || n_quant > cfg->max_seq || n_quant % cfg->group_k != 0 || res_start < 0 ||
+                     res_start >= rows || n_res < 0 || n_res > rows))
+    return KVQ_ERR_INVALID_ARG;
+  if (!res.k_res || !res.v_res || ((((uintptr_t)res.k_res) | ((uintptr_t)res.v_res)) & 15)) return KVQ_ERR_INVALID_ARG;
+  if (!pool.pool_count || !pool.aux_count || !pool.frozen) return KVQ_ERR_INVALID_ARG;
+  if (cfg->outlier_budget > 0 &&
+      (!pool.pool_k || !pool.pool_v || !pool.pool_idx || !pool.pool_score ||
+       ((((uintptr_t)pool.pool_k) | ((uintptr_t)pool.pool_v)) & 15) || (((uintptr_t)pool.pool_idx) & 3) ||
+       (((uintptr_t)pool.pool_score) & 7)))
+    return KVQ_ERR_INVALID_ARG;
+  if (!qcache_ok(cfg, qc) || page_table != qc.page_table) return KVQ_ERR_INVALID_ARG;
+  if (!page_table && (((((uintptr_t)qc.k_codes) | ((uintptr_t)qc.v_codes) | ((uintptr_t)qc.k_meta) | ((uintptr_t)qc.v_meta)) & 15) ||
+                      (((uintptr_t)qc.mask) & 3)))
+    return KVQ_ERR_INVALID_ARG;
+  if (n_pairs > 1024 || (int64_t)cfg->layers * cfg->kv_heads > (1 << 22)) return KVQ_ERR_UNSUPPORTED;
+  Dims d = make_dims(cfg, 0, qc);
+  d.N = cfg->outlier_budget;                             // (of every layer: the untraced ones have no members)
+  return from_hip(kvq::launch_fork(d, cfg->layers, pairs, n_pairs, seq_state, n_quant, res_start, n_res, res, pool, qc,
+                                   page_table, (hipStream_t)stream));
+}
+
+namespace {
+
+// What the calls on pages ask of a pool's live pages.
+int32_t check_live(const kvq_config* cfg, const kvq_qcache& qc, const int32_t* seq_state, int32_t n_quant) {
+  const int32_t st = check_config(cfg);
+  if (st != KVQ_OK) return st;
+  if (!qcache_ok(cfg, qc) || !qc.page_table) return KVQ_ERR_INVALID_ARG;
+  if (((uintptr_t)seq_state) & 15) return KVQ_ERR_INVALID_ARG;
+  if (!seq_state && (n_quant < 0 || n_quant > cfg->max_seq || n_quant % cfg->group_k != 0)) return KVQ_ERR_INVALID_ARG;
+  return KVQ_OK;
+}
+// A pool whose pages are copied (its table plays no part).
+bool pages_ok(const kvq_config* cfg, kvq_qcache qc) {
+  static const int32_t any = 0;
+  qc.page_table = &any;
+  qc.table_stride = cfg->max_seq / cfg->group_k;
+  return qcache_ok(cfg, qc) && (((uintptr_t)qc.mask) & 3) == 0 &&
+         ((((uintptr_t)qc.k_codes) | ((uintptr_t)qc.v_codes) | ((uintptr_t)qc.k_meta) | ((uintptr_t)qc.v_meta)) & 15) == 0;
+}
+
+}  // namespace
+
+int32_t kvq_free_pages(const kvq_config* cfg, kvq_qcache qc, const int32_t* seq_state, int32_t n_quant, int32_t* free_pages,
+                       int32_t* counts, void* stream) {
+  const int32_t st = check_live(cfg, qc, seq_state, n_quant);
+  if (st != KVQ_OK) return st;
+  if (!free_pages || !counts || ((((uintptr_t)free_pages) | ((uintptr_t)counts)) & 3)) return KVQ_ERR_INVALID_ARG;
+  return from_hip(kvq::launch_free_pages(make_dims(cfg, 0, qc), seq_state, n_quant, free_pages, counts, (hipStream_t)stream));
+}
+
+int32_t kvq_copy_pages(const kvq_config* cfg, kvq_qcache from, kvq_qcache to, const int32_t* pairs, int32_t n_pairs,
+                       void* stream) {
+  const int32_t st = check_config(cfg);
+  if (st != KVQ_OK) return st;
+  if (!pages_ok(cfg, from) || !pages_ok(cfg, to)) return KVQ_ERR_INVALID_ARG;
+  if (!pairs || (((uintptr_t)pairs) & 3) || n_pairs < 1) return KVQ_ERR_INVALID_ARG;
+  const int64_t planes = (int64_t)cfg->layers * cfg->kv_heads;
+  if (planes > 0x7FFFFFFF) return KVQ_ERR_UNSUPPORTED;
+  return from_hip(kvq::launch_copy_pages(make_dims(cfg, 0), (int32_t)planes, from, to, pairs, n_pairs, (hipStream_t)stream));
+}
+
+int32_t kvq_compact_pages(const kvq_config* cfg, kvq_qcache from, const int32_t* seq_state, int32_t n_quant, kvq_qcache to,
+                          int32_t* to_table, int32_t* counts, int32_t* workspace, size_t workspace_bytes, void* stream) {
+  const int32_t st = check_live(cfg, from, seq_state, n_quant);
+  if (st != KVQ_OK) return st;
+  if (!pages_ok(cfg, from) || !pages_ok(cfg, to) || to.table_stride < cfg->max_seq / cfg->group_k) return KVQ_ERR_INVALID_ARG;
+  if (from.k_codes == to.k_codes || from.k_meta == to.k_meta || from.v_codes == to.v_codes || from.v_meta == to.v_meta ||
+      from.mask == to.mask || from.page_table == to_table)
+    return KVQ_ERR_INVALID_ARG;
+  if (!to_table || !counts || ((((uintptr_t)to_table) | ((uintptr_t)counts)) & 3)) return KVQ_ERR_INVALID_ARG;
+  if (!workspace || (((uintptr_t)workspace) & 3) || workspace_bytes / 4 < (size_t)from.n_pages) return KVQ_ERR_WORKSPACE;
+  const int64_t planes = (int64_t)cfg->layers * cfg->kv_heads;
+  if (planes > 0x7FFFFFFF) return KVQ_ERR_UNSUPPORTED;
+  return from_hip(kvq::launch_compact_pages(make_dims(cfg, 0, from), (int32_t)planes, from, seq_state, n_quant, to, to_table,
+                                            counts, workspace, (hipStream_t)stream));
+}
+
+namespace {
+
+// The axis of every channel pair, and the arguments that the two calls have in common.
+int32_t check_axes(const kvq_config* cfg, int32_t tokens, const int32_t* positions, int32_t axes, const uint8_t* pair_axis,
+                   const float* freq, kvq::PairAxes* of) {
+  const int32_t st = check_config(cfg);
+  if (st != KVQ_OK) return st;
+  if (tokens < 1 || !positions || (((uintptr_t)positions) & 3) || axes < 1 || axes > 8 || !pair_axis || !freq ||
+      (((uintptr_t)freq) & 3))
+    return KVQ_ERR_INVALID_ARG;
+  for (int i = 0; i < kvq::kHeadDim / 2; ++i) {
+    if (pair_axis[i] >= axes) return KVQ_ERR_INVALID_ARG;
+    of->of[i] = pair_axis[i];
+  }
+  if (tokens > (1 << 26) - 64) return KVQ_ERR_UNSUPPORTED;       // (threads of a launch: 64 per token)
+  return KVQ_OK;
+}
+
+}  // namespace
+
+int32_t kvq_rope_axes(const kvq_config* cfg, const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                      int32_t tokens, const int32_t* positions, int32_t axes, const uint8_t* pair_axis, const float* freq,
+                      void* q_out, int64_t q_out_stride, void* k_out, int64_t k_out_stride, void* stream) {
+  kvq::PairAxes of;
+  const int32_t st = check_axes(cfg, tokens, positions, axes, pair_axis, freq, &of);
+  if (st != KVQ_OK) return st;
+  if ((!q && !k) || (q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr)) return KVQ_ERR_INVALID_ARG;
+  if (q && (!rows_ok(q, q_stride, cfg->q_heads, cfg->head_dim) || !rows_ok(q_out, q_out_stride, cfg->q_heads, cfg->head_dim)))
+    return KVQ_ERR_INVALID_ARG;
+  if (k && (!rows_ok(k, k_stride, cfg->kv_heads, cfg->head_dim) || !rows_ok(k_out, k_out_stride, cfg->kv_heads, cfg->head_dim)))
+    return KVQ_ERR_INVALID_ARG;
+  if ((q && q == q_out && q_stride != q_out_stride) || (k && k == k_out && k_stride != k_out_stride)) return KVQ_ERR_INVALID_ARG;
+  return from_hip(kvq::launch_rope_axes((const __half*)q, q_stride, cfg->q_heads, (const __half*)k, k_stride, cfg->kv_heads,
+                                        tokens, positions, of, freq, (__half*)q_out, q_out_stride, (__half*)k_out,
+                                        k_out_stride, (hipStream_t)stream));
+}
+
+int32_t kvq_rope_rows(const kvq_config* cfg, int32_t tokens, const int32_t* positions, int32_t axes,
+                      const uint8_t* pair_axis, const float* freq, float* rows, void* stream) {
+  kvq::PairAxes of;
+  const int32_t st = check_axes(cfg, tokens, positions, axes, pair_axis, freq, &of);
+  if (st != KVQ_OK) return st;
+  if (!rows || (((uintptr_t)rows) & 15)) return KVQ_ERR_INVALID_ARG;
+  return from_hip(kvq::launch_rope_rows(tokens, positions, of, freq, rows, (hipStream_t)stream));
 }
 
 }  // extern "C"

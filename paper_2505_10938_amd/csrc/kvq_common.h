@@ -135,6 +135,73 @@ struct DecodeArgs {
   int64_t rope_stride;
 };
 
+// A chunk of new tokens against the caches of a batch (and against itself).
+constexpr int kChunkRows = 128;        // query rows, (token, query head) pairs of a kv head, of one workgroup
+struct ChunkArgs {
+  Dims d;
+  const __half* q;
+  const __half* k_new;                  // null: no new tokens, every query sees the whole cache
+  const __half* v_new;
+  __half* out;
+  int64_t q_stride, kv_stride;          // elements from token to token
+  const int32_t* starts;                // [batch + 1] or null (see kvq_chunk)
+  int32_t total, max_tokens;
+  const uint8_t* k_codes;               // the whole arrays (paged: pools of pages)
+  const uint8_t* k_meta;
+  const uint8_t* v_codes;
+  const uint8_t* v_meta;
+  const uint32_t* mask;
+  const __half* k_res;
+  const __half* v_res;
+  const __half* pool_k;
+  const __half* pool_v;
+  const int32_t* pool_count;
+  const int32_t* aux_count;
+  const int32_t* seq;                   // per-sequence state, or null; with it n_quant and n_res are upper bounds
+  int32_t n_quant, res_start, n_res;
+  int32_t g_shift;                      // query heads per kv head = 1 << g_shift
+  float scale;                          // 1 / sqrt(head_dim) * log2(e): scores are kept in powers of two
+  int32_t row_tiles;                    // workgroups per unit along the query rows, of max_tokens tokens
+  int32_t splits;                       // workgroups that share a row tile's keys
+  uint32_t items;                       // units * row_tiles * splits
+  float* share_ml;                      // splits > 1: [unit][row][split][2] maximum (log2) and sum of a row's share
+  float* share_o;                       //             [unit][row][split][head_dim]
+};
+
+hipError_t launch_prompt_attention(const ChunkArgs& a, hipStream_t s);
+
+// Sequence b's rows of a chunk's packed arrays.
+struct ChunkRows {
+  int64_t first;
+  int32_t n;
+};
+__device__ __forceinline__ ChunkRows chunk_rows(const int32_t* starts, int32_t total, int32_t max_tokens, int b) {
+  if (!starts) return {(int64_t)b * max_tokens, max_tokens};
+  const int lo = min(max(starts[b], 0), total), hi = min(max(starts[b + 1], lo), total);
+  return {lo, min(hi - lo, max_tokens)};
+}
+
+struct PairAxes {
+  uint8_t of[kHeadDim / 2];
+};
+hipError_t launch_rope_axes(const __half* q, int64_t q_stride, int32_t q_heads, const __half* k, int64_t k_stride,
+                            int32_t k_heads, int32_t tokens, const int32_t* positions, const PairAxes& axes, const float* freq,
+                            __half* q_out, int64_t q_out_stride, __half* k_out, int64_t k_out_stride, hipStream_t s);
+hipError_t launch_rope_rows(int32_t tokens, const int32_t* positions, const PairAxes& axes, const float* freq, float* rows,
+                            hipStream_t s);
+hipError_t launch_fork(const Dims& d, int32_t layers, const int32_t* pairs, int32_t n_pairs, int32_t* seq, int32_t n_quant,
+                       int32_t res_start, int32_t n_res, const kvq_residual& res, const kvq_pool& pool,
+                       const kvq_qcache& qc, int32_t* page_table, hipStream_t s);
+hipError_t launch_free_pages(const Dims& d, const int32_t* seq, int32_t n_quant, int32_t* free_pages, int32_t* counts,
+                             hipStream_t s);
+hipError_t launch_copy_pages(const Dims& d, int32_t planes, const kvq_qcache& from, const kvq_qcache& to, const int32_t* pairs,
+                             int32_t n_pairs, hipStream_t s);
+hipError_t launch_compact_pages(const Dims& d, int32_t planes, const kvq_qcache& from, const int32_t* seq, int32_t n_quant,
+                                const kvq_qcache& to, int32_t* to_table, int32_t* counts, int32_t* sources, hipStream_t s);
+hipError_t launch_extend(const Dims& d, const __half* k_new, const __half* v_new, int64_t kv_stride, const kvq_chunk& chunk,
+                         const kvq_residual& res, const int32_t* seq, int32_t n_quant, int32_t res_start, int32_t n_res,
+                         const kvq_pool& pool, uint8_t* selected, const kvq_qcache& qc, hipStream_t s);
+hipError_t launch_seq_extend(const Dims& d, int32_t* seq, const kvq_chunk& chunk, hipStream_t s);
 hipError_t launch_append(const Dims& d, const __half* k_new, const __half* v_new, __half* k_res, __half* v_res,
                          int32_t row, hipStream_t s);
 hipError_t launch_dequantize(const Dims& d, int32_t block0, int32_t n_blocks, const kvq_qcache& qc, const kvq_pool& pool,
@@ -194,6 +261,22 @@ __device__ __forceinline__ int wave_scan(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x142 /* row_bcast:15 */, 0xa, 0xf, false);
   v += __builtin_amdgcn_update_dpp(0, v, 0x143 /* row_bcast:31 */, 0xc, 0xf, false);
   return v;
+}
+
+// Rotary position embedding of one lane's channel pair (2*lane, 2*lane + 1).  Channel i < 64 forms a
+// plane with channel i + 64, so a lane's partner is lane ^ 32 and both use the angles of pair lane & 31:
+//     y_i = x_i cos_i - x_{i+64} sin_i,   y_{i+64} = x_{i+64} cos_i + x_i sin_i
+// (Su et al., "RoFormer", Eq. 34, in the half-split pairing).  Each product and the sum are rounded to
+// fp32 on their own and the result once to fp16: the rotated Key row is stored, and what is stored must
+// not depend on how a compiler contracts the expression.
+__device__ inline uint32_t rope_word(uint32_t own, uint32_t partner, float2 c, float2 s, bool upper) {
+#pragma clang fp contract(off)
+  const float o0 = __half2float(__ushort_as_half((unsigned short)(own & 0xFFFFu))), o1 = __half2float(__ushort_as_half((unsigned short)(own >> 16)));
+  const float p0 = __half2float(__ushort_as_half((unsigned short)(partner & 0xFFFFu))), p1 = __half2float(__ushort_as_half((unsigned short)(partner >> 16)));
+  const float a0 = o0 * c.x, a1 = o1 * c.y, b0 = p0 * s.x, b1 = p1 * s.y;
+  const float y0 = upper ? a0 + b0 : a0 - b0;
+  const float y1 = upper ? a1 + b1 : a1 - b1;
+  return (uint32_t)__half_as_ushort(__float2half_rn(y0)) | ((uint32_t)__half_as_ushort(__float2half_rn(y1)) << 16);
 }
 
 // ---- packed layout ---------------------------------------------------------------------------

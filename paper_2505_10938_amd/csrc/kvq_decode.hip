@@ -176,22 +176,6 @@ __device__ inline void mul_split(half2v ah, half2v al, half2v b, uint32_t& hi, u
 }
 __device__ inline half2v as_half2(uint32_t w) { return __builtin_bit_cast(half2v, w); }
 
-// Rotary position embedding of one lane's channel pair (2*lane, 2*lane + 1).  Channel i < 64 forms a
-// plane with channel i + 64, so a lane's partner is lane ^ 32 and both use the angles of pair lane & 31:
-//     y_i = x_i cos_i - x_{i+64} sin_i,   y_{i+64} = x_{i+64} cos_i + x_i sin_i
-// (Su et al., "RoFormer", Eq. 34, in the half-split pairing).  Each product and the sum are rounded to
-// fp32 on their own and the result once to fp16: the rotated Key row is stored, and what is stored must
-// not depend on how a compiler contracts the expression.
-__device__ inline uint32_t rope_word(uint32_t own, uint32_t partner, float2 c, float2 s, bool upper) {
-#pragma clang fp contract(off)
-  const float o0 = h2f_bits(own & 0xFFFFu), o1 = h2f_bits(own >> 16);
-  const float p0 = h2f_bits(partner & 0xFFFFu), p1 = h2f_bits(partner >> 16);
-  const float a0 = o0 * c.x, a1 = o1 * c.y, b0 = p0 * s.x, b1 = p1 * s.y;
-  const float y0 = upper ? a0 + b0 : a0 - b0;
-  const float y1 = upper ? a1 + b1 : a1 - b1;
-  return (uint32_t)__half_as_ushort(__float2half_rn(y0)) | ((uint32_t)__half_as_ushort(__float2half_rn(y1)) << 16);
-}
-
 // Exponent of the power of two carried by pair v (v = lane & 3 on the producing side) of a
 // field: a masked code at pair v is worth code * 2^(pos(v) - 24).
 template <int BITS>

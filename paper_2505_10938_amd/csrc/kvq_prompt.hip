@@ -1,0 +1,543 @@
+// Attention of a chunk of new tokens over a sequence's low-bit cache and, causally, over itself (Eq. 1 over the sets of
+// the decode step, and the prefill phase's attention among the prompt's own tokens).
+#include "kvq_common.h"
+
+#include <type_traits>
+
+namespace kvq {
+
+namespace {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef __fp16 lds_half4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) lds_half4* lds_half4_ptr;
+typedef float float16v __attribute__((ext_vector_type(16)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kTile = 64;            // keys per tile
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kWaveRows = 32;        // query rows of a wavefront: (token, query head) pairs, token-major
+constexpr int kRows = kChunkRows;
+static_assert(kRows == kWaves * kWaveRows, "a workgroup's rows are its wavefronts'");
+constexpr int kPitchK = 272;         // LDS rows of 128 fp16: 16 bytes more, so that 16 rows' 16-byte pieces lie in different banks
+constexpr int kPitchV = 320;         // four rows' 64-byte pieces in different banks
+constexpr int kPitchT = 144;         // LDS rows of 64 keys of one channel
+constexpr int kBytesK = kTile * kPitchK;
+constexpr int kBytesV = kTile * kPitchV > kHeadDim * kPitchT ? kTile * kPitchV : kHeadDim * kPitchT;
+constexpr int kBytesBuffer = kBytesK + kBytesV;
+// A row's weights are taken relative to a maximum that may lie below the true one by this much (powers of two), so that
+// the outputs are rescaled only when it has grown by more.  Weights up to 2^8 keep their 11 bits in fp16.
+constexpr float kSlack = 8.0f;
+
+__device__ __forceinline__ half2v as_h2(uint32_t w) { return __builtin_bit_cast(half2v, w); }
+__device__ __forceinline__ uint32_t as_u32(half2v v) { return __builtin_bit_cast(uint32_t, v); }
+__device__ __forceinline__ uint32_t rotr32(uint32_t w, int n) { return __builtin_amdgcn_alignbit(w, w, n); }
+
+// The four code pairs (x = 2v, 2v + 1 in the two halves) of a field as fp16 numbers zero + code * step, one rounding each.
+// `w` is the field's word, rotated so that the pairs v = 0 .. (2-bit: all, 4-bit: 0 and 1, and 2 and 3 eight bits further)
+// stand at bits 2.. of each half.  A code at bit p of the significand of 2^(10 - p) is worth itself.
+template <int BITS, int V>
+__device__ __forceinline__ uint32_t dequant_pair(uint32_t w, uint32_t step, uint32_t zero) {
+  constexpr int p = BITS == 2 ? 2 * (V + 1) : 2 + 4 * (V & 1);
+  constexpr uint32_t mask = (uint32_t)((1 << BITS) - 1) << p, one = (uint32_t)(25 - p) << 10;
+  const uint32_t x = (w & (mask | (mask << 16))) | (one | (one << 16));
+  constexpr _Float16 base = (_Float16)(float)(1 << (10 - p));
+  const half2v code = as_h2(x) - half2v{base, base};
+  return as_u32(__builtin_elementwise_fma(code, as_h2(step), as_h2(zero)));
+}
+template <int BITS>
+__device__ __forceinline__ u32x4 dequant_field(const uint32_t (&w)[2 * BITS], int f, const uint32_t (&step)[4],
+                                               const uint32_t (&zero)[4]) {
+  u32x4 r;
+  if (BITS == 2) {
+    const uint32_t word = (f & 1) ? rotr32(w[f >> 1], 8) : w[f >> 1];
+    r[0] = dequant_pair<2, 0>(word, step[0], zero[0]);
+    r[1] = dequant_pair<2, 1>(word, step[1], zero[1]);
+    r[2] = dequant_pair<2, 2>(word, step[2], zero[2]);
+    r[3] = dequant_pair<2, 3>(word, step[3], zero[3]);
+  } else {
+    const uint32_t word = w[f], high = rotr32(word, 8);
+    r[0] = dequant_pair<4, 0>(word, step[0], zero[0]);
+    r[1] = dequant_pair<4, 1>(word, step[1], zero[1]);
+    r[2] = dequant_pair<4, 2>(high, step[2], zero[2]);
+    r[3] = dequant_pair<4, 3>(high, step[3], zero[3]);
+  }
+  return r;
+}
+
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {      // either half an infinity or a NaN
+  return ((w & 0x7C00u) == 0x7C00u) | ((w & 0x7C000000u) == 0x7C000000u);
+}
+
+// The value of lane ^ 32.
+__device__ __forceinline__ float other_half(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
+}
+
+// What a wavefront loads for the next tile of quantized tokens: one block's Keys (wavefronts 0, 1) or Values (2, 3).
+template <int BITS, int NV>
+struct QuantRegs {
+  u32x4 codes[BITS / 2];
+  u32x4 step[4], zero[4];              // Keys: of the channels of the lane's four fields; Values: [pair][value group]
+};
+
+// One wavefront has 32 query rows, whose products with 64 keys stand transposed in its registers (keys down, one query row
+// per lane and half): the softmax of a row is then work inside a lane, and the weights are, as they stand, an operand of the
+// second product if its keys are taken in the order in which the first one leaves them (16 s + 8 (j / 4) + 4 h + j % 4 for half
+// h of the lanes, element j).  Four wavefronts share the keys' and values' tiles in LDS, two buffers.
+template <int BITS, int NV>
+__global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs a) {
+  extern __shared__ __align__(16) unsigned char smem[];
+  const Dims& d = a.d;
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+
+  // ---- which rows, which keys
+  // Workgroups go round the eight XCDs; each takes a run of neighbouring work items, so that those that share a unit's
+  // keys share an L2 cache as well.
+  const uint32_t per_xcd = gridDim.x >> 3;
+  const uint32_t item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+  if (item >= a.items) return;
+  const uint32_t per_unit = a.row_tiles * a.splits;
+  const int ul = item / per_unit;
+  const uint32_t in_unit = item - ul * per_unit;
+  const int tile_back = in_unit / a.splits, split = in_unit - tile_back * a.splits;
+  const int b = ul / d.kv_heads, h = ul - b * d.kv_heads;
+  const ChunkRows mine = chunk_rows(a.starts, a.total, a.max_tokens, b);
+  const int64_t s0 = mine.first;
+  const int n = mine.n;
+  const int row_tiles = (int)(((int64_t)n * d.g + kRows - 1) / kRows);
+  if (tile_back >= row_tiles) return;
+  const int row_tile = row_tiles - 1 - tile_back;        // the longest ones first
+  int nq = a.n_quant, rs = a.res_start, nr = a.n_res;
+  if (a.seq) {
+    const int4 own = *(const int4*)(a.seq + 4 * b);
+    nq = min(max(own.x, 0), a.n_quant) & ~(kBlockTokens - 1);
+    rs = (own.y >= 0 && own.y < d.res_rows) ? own.y : 0;
+    nr = min(max(own.z, 0), a.n_res);
+  }
+  const int64_t u = d.unit0 + ul;
+  const int n_pool = d.N > 0 ? min(max(a.pool_count[u], 0), d.N) : 0;
+  const int n_aux = d.N > 0 ? min(max(a.aux_count[u], 0), d.A) : 0;
+  const int n_rows = n_pool + n_aux + nr;                // full-precision rows of the cache
+  const int first_row = row_tile * kRows;                // of the unit's n * g rows
+  const int live_rows = (int)min((int64_t)kRows, (int64_t)n * d.g - first_row);
+  const int first_token = first_row >> a.g_shift;
+  const int n_new = a.k_new ? min(n, ((first_row + live_rows - 1) >> a.g_shift) + 1) : 0;
+  const int tq = (nq + kTile - 1) / kTile, tr = (n_rows + kTile - 1) / kTile, tn = (n_new + kTile - 1) / kTile;
+  const int tiles = tq + tr + tn;
+  const int per = (tiles + a.splits - 1) / a.splits;
+  const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
+
+  // ---- the wavefront's query rows, as a matrix operand: lane (row col, channels 16 s + 8 half ..)
+  const int wave_row = first_row + wave * kWaveRows;
+  const bool wave_live = wave * kWaveRows < live_rows;
+  const int row = wave_row + col;
+  const bool row_live = wave * kWaveRows + col < live_rows;
+  const int token = row >> a.g_shift, head = h * d.g + (row & (d.g - 1));
+  half8 q[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s) q[s] = half8{0, 0, 0, 0, 0, 0, 0, 0};
+  if (row_live) {
+    const __half* qr = a.q + (s0 + token) * a.q_stride + head * kHeadDim + 8 * half;
+#pragma unroll
+    for (int s = 0; s < 8; ++s) q[s] = *(const half8*)(qr + 16 * s);
+  }
+
+  float16v o[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[c][r] = 0.0f;
+  float m = kNegBig, l = 0.0f;                           // of the lane's row: maximum (log2), sum over the half's keys
+
+  unsigned char* buffer = smem;
+  auto other = [&](unsigned char* p) { return smem + (p == smem ? kBytesBuffer : 0); };
+
+  // First product, softmax, second product of one tile.  `limit`: keys of the tile below it are seen by the lane's row;
+  // `hidden`: blocks' mask words (quantized tiles).  V stands as rows of channels (two transposing reads bring four keys each of a channel to
+  // a lane) or, dequantized, already by channel in the order of the second product.
+  auto compute = [&](auto quantized, const unsigned char* buf, int limit, bool all, uint32_t hidden0, uint32_t hidden1,
+                     float (&p)[2][16]) {
+    constexpr bool QUANT = decltype(quantized)::value;
+    const unsigned char* sk = buf + col * kPitchK + 16 * half;
+    float16v x[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) x[t][r] = 0.0f;
+#pragma unroll
+      for (int s = 0; s < 8; ++s)
+        x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)(sk + 32 * t * kPitchK + 32 * s), q[s], x[t], 0, 0, 0);
+    }
+    if (QUANT) {
+      if (hidden0 | hidden1) {                           // uniform
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const uint32_t word = (t ? hidden1 : hidden0) >> (4 * half);
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (word & (1u << (8 * (r >> 2) + (r & 3)))) x[t][r] = -__builtin_inff();
+        }
+      }
+    } else if (!all) {                                   // uniform
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (32 * t + 8 * (r >> 2) + (r & 3) + 4 * half >= limit) x[t][r] = -__builtin_inff();
+    }
+    float top = fmaxf(x[0][0], x[1][0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) top = fmaxf(top, fmaxf(x[0][r], x[1][r]));
+    top = fmaxf(top, other_half(top)) * a.scale;
+    if (__any(top > m + kSlack)) {
+      const float m_new = fmaxf(m, top);
+      const float down = __builtin_amdgcn_exp2f(m - m_new);
+      m = m_new;
+      l *= down;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[c][r] *= down;
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        p[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], a.scale, -m));
+        sum += p[t][r];
+      }
+    l += sum;
+    const unsigned char* sv = buf + kBytesK;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      half8 w;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = (_Float16)p[s >> 1][8 * (s & 1) + j];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        half8 v;
+        if (QUANT) {
+          v = *(const half8*)(sv + (32 * c + col) * kPitchT + 32 * s + 16 * half);
+        } else {
+          const unsigned char* at = sv + (16 * s + 4 * half + ((lane & 15) >> 2)) * kPitchV + 2 * (32 * c + (lane & 16) + 4 * (lane & 3));
+          const half4 lo = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_half4_ptr)at));
+          const half4 hi = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_half4_ptr)(at + 8 * kPitchV)));
+          v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w, o[c], 0, 0, 0);
+      }
+    }
+  };
+
+  // ---- quantized tokens, 64 (two blocks) a tile: each wavefront turns one block's Keys or Values into fp16 rows
+  {
+    const int which = wave >> 1;                         // 0: Keys, 1: Values
+    const int last = (nq >> 5) - 1;
+    const int qe = min(t_end, tq);
+    const int r = lane >> 4, m16 = lane & 15;
+    QuantRegs<BITS, NV> R;
+    uint32_t mask0 = 0, mask1 = 0;
+    auto place = [&](int blk) {                          // (one block behind the last: the last one again, all of it hidden)
+      const GroupPlace at = place_of_group(d, ul, blk >> d.bpg_shift);
+      return at;
+    };
+    auto load = [&](int tile) {
+      const int blk = min(2 * tile + (wave & 1), last);
+      const GroupPlace at = place(blk);
+      const int64_t pblk = at.row * d.blocks_per_unit + ((int64_t)at.slot << d.bpg_shift) + (blk & ((1 << d.bpg_shift) - 1));
+      const u32x4* codes = (const u32x4*)((which ? a.v_codes : a.k_codes) + pblk * d.block_bytes);
+#pragma unroll
+      for (int i = 0; i < BITS / 2; ++i) R.codes[i] = codes[64 * i + lane];
+      if (which == 0) {
+        const unsigned char* meta = a.k_meta + (at.row * d.groups_per_unit + at.slot) * 512 + 16 * r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          R.step[i] = *(const u32x4*)(meta + 64 * i);
+          R.zero[i] = *(const u32x4*)(meta + 64 * i + 256);
+        }
+      } else {
+        const unsigned char* meta = a.v_meta + pblk * (128 * NV) + 16 * NV * r;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+          R.step[i] = *(const u32x4*)(meta + 16 * i);
+          R.zero[i] = *(const u32x4*)(meta + 16 * i + 64 * NV);
+        }
+      }
+      // (every wavefront wants both blocks' mask words)
+      const int b0 = 2 * tile, b1 = min(2 * tile + 1, last);
+      const GroupPlace g0 = place(b0), g1 = place(b1);
+      const int in_group = (1 << d.bpg_shift) - 1;
+      mask0 = a.mask[g0.row * d.blocks_per_unit + ((int64_t)g0.slot << d.bpg_shift) + (b0 & in_group)];
+      mask1 = a.mask[g1.row * d.blocks_per_unit + ((int64_t)g1.slot << d.bpg_shift) + (b1 & in_group)];
+      if (2 * tile + 1 > last) mask1 = ~0u;
+    };
+    auto store = [&](unsigned char* buf) {
+      const int at = 32 * (wave & 1);                    // the block's tokens of the tile
+      uint32_t w[2 * BITS];
+#pragma unroll
+      for (int i = 0; i < 2 * BITS; ++i) w[i] = R.codes[i >> 2][i & 3];
+      if (which == 0) {                                  // field 4 th + cb: 8 channels from 32 cb + 8 r on of token 16 th + m16
+        unsigned char* sk = buf + (at + m16) * kPitchK + 16 * r;
+#pragma unroll
+        for (int f = 0; f < 8; ++f) {
+          uint32_t st[4], ze[4];
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            st[v] = R.step[f & 3][v];
+            ze[v] = R.zero[f & 3][v];
+          }
+          *(u32x4*)(sk + 16 * (f >> 2) * kPitchK + 64 * (f & 3)) = dequant_field<BITS>(w, f, st, ze);
+        }
+      } else {                                           // field ct: tokens 8 r .. of channel 16 ct + m16
+        unsigned char* sv = buf + kBytesK + m16 * kPitchT + 2 * (at + 16 * (r >> 1) + 4 * (r & 1));
+#pragma unroll
+        for (int f = 0; f < 8; ++f) {
+          constexpr int kFieldsPerGroup = 8 / NV;
+          uint32_t st[4], ze[4];
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int i = v * NV + f / kFieldsPerGroup;
+            st[v] = R.step[i >> 2][i & 3];
+            ze[v] = R.zero[i >> 2][i & 3];
+          }
+          const u32x4 x = dequant_field<BITS>(w, f, st, ze);
+          *(u32x2*)(sv + 16 * f * kPitchT) = u32x2{x[0], x[1]};
+          *(u32x2*)(sv + 16 * f * kPitchT + 16) = u32x2{x[2], x[3]};
+        }
+      }
+    };
+    if (t_begin < qe) {
+      load(t_begin);
+      uint32_t h0 = mask0, h1 = mask1;
+      store(buffer);
+      __syncthreads();
+      for (int t = t_begin; t < qe; ++t) {
+        const bool more = t + 1 < qe;
+        if (more) load(t + 1);
+        float p[2][16];
+        if (wave_live) compute(std::true_type{}, buffer, kTile, true, __builtin_amdgcn_readfirstlane(h0), __builtin_amdgcn_readfirstlane(h1), p);
+        buffer = other(buffer);
+        if (more) {
+          h0 = mask0;
+          h1 = mask1;
+          store(buffer);
+        }
+        __syncthreads();
+      }
+    }
+  }
+
+  // ---- full-precision rows, 64 a tile: the pools' members and the ring, then the new tokens
+  {
+    const int fb = max(t_begin, tq);
+    const int piece = tid & 15, line = tid >> 4;
+    u32x4 rk[4], rv[4];
+    const __half* pk = a.pool_k + u * d.pool_slots * kHeadDim + 8 * piece;
+    const __half* pv = a.pool_v + u * d.pool_slots * kHeadDim + 8 * piece;
+    const __half* ck = a.k_res + u * d.res_rows * kHeadDim + 8 * piece;
+    const __half* cv = a.v_res + u * d.res_rows * kHeadDim + 8 * piece;
+    const __half* nk = a.k_new + s0 * a.kv_stride + h * kHeadDim + 8 * piece;
+    const __half* nv = a.v_new + s0 * a.kv_stride + h * kHeadDim + 8 * piece;
+    auto load = [&](int tile) {
+      const u32x4 none = {0, 0, 0, 0};
+      if (tile < tq + tr) {                              // uniform
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = (tile - tq) * kTile + 16 * i + line;
+          rk[i] = rv[i] = none;
+          if (e < n_rows) {
+            int at = e < n_pool ? e : d.pool_slots - d.A + (e - n_pool);
+            if (e >= n_pool + n_aux) {
+              at = rs + (e - n_pool - n_aux);
+              at -= at >= d.res_rows ? d.res_rows : 0;
+              rk[i] = *(const u32x4*)(ck + at * kHeadDim);
+              rv[i] = *(const u32x4*)(cv + at * kHeadDim);
+            } else {
+              rk[i] = *(const u32x4*)(pk + at * kHeadDim);
+              rv[i] = *(const u32x4*)(pv + at * kHeadDim);
+            }
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int e = (tile - tq - tr) * kTile + 16 * i + line;
+          rk[i] = rv[i] = none;
+          if (e < n_new) {
+            rk[i] = *(const u32x4*)(nk + e * a.kv_stride);
+            rv[i] = *(const u32x4*)(nv + e * a.kv_stride);
+          }
+        }
+      }
+    };
+    // Where some rows see a new token and others do not, its Value must not reach the others, for 0 times an infinity is a
+    // NaN: what is not finite is left out of the tile (and counted in by `late` for the rows that see it).
+    auto store = [&](unsigned char* buf, bool partly) {
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (partly) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t bad = not_finite(rv[i][k]);
+            odd |= bad;
+            const uint32_t w = rv[i][k];
+            rv[i][k] = ((w & 0x7C00u) == 0x7C00u ? 0u : w & 0xFFFFu) | ((w & 0x7C000000u) == 0x7C000000u ? 0u : w & 0xFFFF0000u);
+          }
+        }
+        *(u32x4*)(buf + (16 * i + line) * kPitchK + 16 * piece) = rk[i];
+        *(u32x4*)(buf + kBytesK + (16 * i + line) * kPitchV + 16 * piece) = rv[i];
+      }
+      return odd;
+    };
+    auto seen_partly = [&](int tile) { return tile >= tq + tr && (tile - tq - tr + 1) * kTile - 1 > first_token; };
+    // The Values left out of a tile, for the rows that see them.  Weights go through LDS (the buffer that is not in use).
+    auto late = [&](int tile, int limit, unsigned char* spare, const float (&p)[2][16]) {
+      float* mine = (float*)(spare + wave * (kWaveRows * kTile * 4));
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mine[(32 * t + 8 * (r >> 2) + 4 * half + (r & 3)) * kWaveRows + col] = p[t][r];
+      __builtin_amdgcn_s_waitcnt(0xc07f);                // lgkmcnt(0): the wavefront's own stores
+      __builtin_amdgcn_wave_barrier();
+      const int base = (tile - tq - tr) * kTile;
+      for (int k = 0; k < kTile && base + k < n_new; ++k) {
+        const float w = mine[k * kWaveRows + col];
+        const __half* vr = a.v_new + (s0 + base + k) * a.kv_stride + h * kHeadDim + 4 * half;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const half4 v = *(const half4*)(vr + 32 * c + 8 * r4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (k < limit && w != 0.0f && !(fabsf((float)v[i]) <= 65504.0f)) o[c][4 * r4 + i] += w * (float)v[i];
+          }
+      }
+    };
+    if (fb < t_end) {
+      load(fb);
+      bool odd = __syncthreads_or(store(buffer, seen_partly(fb)));
+      for (int t = fb; t < t_end; ++t) {
+        const bool more = t + 1 < t_end;
+        if (more) load(t + 1);
+        // how many of the tile's keys the lane's row sees, and whether every row of the wavefront sees all
+        const bool own_new = t >= tq + tr;
+        const int base = own_new ? (t - tq - tr) * kTile : (t - tq) * kTile;
+        const int limit = (own_new ? min(n_new, token + 1) : n_rows) - base;
+        const int least = (own_new ? min(n_new, (wave_row >> a.g_shift) + 1) : n_rows) - base;
+        const int most = (own_new ? min(n_new, ((wave_row + kWaveRows - 1) >> a.g_shift) + 1) : n_rows) - base;
+        if (wave_live && most > 0) {
+          float p[2][16];
+          compute(std::false_type{}, buffer, limit, least >= kTile, 0u, 0u, p);
+          if (odd) late(t, limit, other(buffer), p);
+        }
+        buffer = other(buffer);
+        if (more) {
+          const bool partly = seen_partly(t + 1);
+          if (odd) __syncthreads();                      // (the weights' place in the other buffer)
+          const uint32_t found = store(buffer, partly);
+          if (partly) odd = __syncthreads_or(found);
+          else { __syncthreads(); odd = false; }
+        }
+      }
+    }
+  }
+
+  // ---- the rows' results: normalized, or this split's share
+  if (!row_live) return;
+  l += other_half(l);
+  if (a.splits == 1) {
+    const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+    __half* to = a.out + ((s0 + token) * d.q_heads + head) * kHeadDim + 4 * half;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int r4 = 0; r4 < 4; ++r4) {
+        half4 y;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = (_Float16)(o[c][4 * r4 + i] * inv);
+        *(half4*)(to + 32 * c + 8 * r4) = y;
+      }
+    return;
+  }
+  const int64_t place = (((int64_t)ul * a.row_tiles + row_tile) * kRows + (row - first_row)) * a.splits + split;
+  if (half == 0) *(float2*)(a.share_ml + 2 * place) = make_float2(m, l);
+  if (l == 0.0f) return;
+  float* to = a.share_o + place * kHeadDim + 4 * half;
+#pragma unroll
+  for (int c = 0; c < 4; ++c)
+#pragma unroll
+    for (int r4 = 0; r4 < 4; ++r4)
+      *(float4*)(to + 32 * c + 8 * r4) = make_float4(o[c][4 * r4], o[c][4 * r4 + 1], o[c][4 * r4 + 2], o[c][4 * r4 + 3]);
+}
+
+// The shares of a row's splits put together: sum of 2^(m_i - max m) (l_i, o_i).  32 lanes a row.
+__global__ void __launch_bounds__(kThreads) prompt_merge_kernel(ChunkArgs a) {
+  const Dims& d = a.d;
+  const int sub = threadIdx.x & 31;
+  const int row = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  const int h = blockIdx.y, b = blockIdx.z, ul = b * d.kv_heads + h;
+  const ChunkRows mine = chunk_rows(a.starts, a.total, a.max_tokens, b);
+  const int64_t s0 = mine.first;
+  const int n = mine.n;
+  if (row >= (int64_t)n * d.g) return;
+  const int64_t place = ((int64_t)ul * a.row_tiles * kRows + row) * a.splits;
+  const float* ml = a.share_ml + 2 * place;
+  float m = kNegBig;
+  for (int i = 0; i < a.splits; ++i)
+    if (ml[2 * i + 1] != 0.0f) m = fmaxf(m, ml[2 * i]);
+  float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int i = 0; i < a.splits; ++i) {
+    const float li = ml[2 * i + 1];
+    if (li == 0.0f) continue;                            // (this share saw nothing, and left no rows)
+    const float w = __builtin_amdgcn_exp2f(ml[2 * i] - m);
+    const float4 x = *(const float4*)(a.share_o + (place + i) * kHeadDim + 4 * sub);
+    l += w * li;
+    o[0] += w * x.x;
+    o[1] += w * x.y;
+    o[2] += w * x.z;
+    o[3] += w * x.w;
+  }
+  const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+  half4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = (_Float16)(o[i] * inv);
+  const int token = row >> a.g_shift, head = h * d.g + (row & (d.g - 1));
+  *(half4*)(a.out + ((s0 + token) * d.q_heads + head) * kHeadDim + 4 * sub) = y;
+}
+
+}  // namespace
+
+hipError_t launch_prompt_attention(const ChunkArgs& a, hipStream_t s) {
+  const uint32_t grid = (a.items + 7) / 8 * 8;
+  auto go = [&](auto kern) {
+    hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kBytesBuffer);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), 2 * kBytesBuffer, s, a);
+    return hipGetLastError();
+  };
+  auto of_bits = [&](auto bits) {
+    constexpr int BITS = decltype(bits)::value;
+    switch (a.d.vgroups) {
+      case 4: return go(prompt_attention_kernel<BITS, 4>);
+      case 2: return go(prompt_attention_kernel<BITS, 2>);
+      default: return go(prompt_attention_kernel<BITS, 1>);
+    }
+  };
+  hipError_t e = a.d.bits == 2 ? of_bits(std::integral_constant<int, 2>{}) : of_bits(std::integral_constant<int, 4>{});
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t rows = (int64_t)a.max_tokens * a.d.g;
+  hipLaunchKernelGGL(prompt_merge_kernel, dim3((uint32_t)((rows + 7) / 8), a.d.kv_heads, a.d.batch), dim3(kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace kvq

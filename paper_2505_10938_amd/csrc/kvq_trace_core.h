@@ -57,6 +57,14 @@ __device__ inline UnitPool unit_pool(const Dims& d, int64_t u, __half* pool_k, _
   return p;
 }
 
+// Where a group's rows are: `k(t)`, `v(t)` of token t.  Behind each other:
+struct GroupOf {
+  const __half* gk;
+  const __half* gv;
+  __device__ __forceinline__ const __half* k(int t) const { return gk + t * kHeadDim; }
+  __device__ __forceinline__ const __half* v(int t) const { return gv + t * kHeadDim; }
+};
+
 // What the first phase loads.
 template <int G>
 struct Loaded {
@@ -73,9 +81,9 @@ constexpr int kPoolRowsAhead = 16;
 
 // Issue every load of the first phase (state, stored scores, the group's Key rows); nothing is
 // waited for here.  Rows are handled by teams of 16 lanes (16 bytes per lane).  Requires N > 0.
-template <int G>
-__device__ __forceinline__ void load(Loaded<G>& in, const Dims& d, const UnitPool& p, const __half* gk, int tid,
-                                     bool pool_rows_ahead = false) {
+template <int G, class Rows>
+__device__ __forceinline__ void load_from(Loaded<G>& in, const Dims& d, const UnitPool& p, const Rows& rows, int tid,
+                                          bool pool_rows_ahead = false) {
   in.is_frozen = *p.frozen;
   in.n_old = *p.pool_count;
   in.n_aux = *p.aux_count;
@@ -88,12 +96,18 @@ __device__ __forceinline__ void load(Loaded<G>& in, const Dims& d, const UnitPoo
   const int team = (tid & (kWorkers - 1)) >> 4, sub = tid & 15;
   if (tid < kWorkers) {
 #pragma unroll
-    for (int q = 0; q < G / 16; ++q) in.kr[q] = *(const uint4*)(gk + (q * 16 + team) * kHeadDim + sub * 8);
+    for (int q = 0; q < G / 16; ++q) in.kr[q] = *(const uint4*)(rows.k(q * 16 + team) + sub * 8);
     if (pool_rows_ahead && team < d.N) {               // d.N <= kPoolRowsAhead: one slot per team
       in.pool_kr = *(const uint4*)(p.pk + (int64_t)team * kHeadDim + sub * 8);
       in.pool_vr = *(const uint4*)(p.pv + (int64_t)team * kHeadDim + sub * 8);
     }
   }
+}
+
+template <int G>
+__device__ __forceinline__ void load(Loaded<G>& in, const Dims& d, const UnitPool& p, const __half* gk, int tid,
+                                     bool pool_rows_ahead = false) {
+  load_from<G>(in, d, p, GroupOf{gk, nullptr}, tid, pool_rows_ahead);
 }
 
 // The competition and the pool update.  Every thread of the workgroup must call it (it holds
@@ -103,11 +117,11 @@ __device__ __forceinline__ void load(Loaded<G>& in, const Dims& d, const UnitPoo
 // `staged_k`, `staged_v` (may be null): the group's rows in LDS, row t at byte t * staged_pitch; with them,
 // and with the pool rows fetched ahead (`pool_rows_ahead`, as passed to load()), no moving row is read
 // from memory.
-template <int G>
-__device__ __forceinline__ void compete(Loaded<G>& in, const Dims& d, int group_index, const UnitPool& p,
-                                        const __half* gk, const __half* gv, uint8_t* sel, uint8_t* sel_lds, int tid,
-                                        const unsigned char* staged_k = nullptr, const unsigned char* staged_v = nullptr,
-                                        int staged_pitch = 0, bool pool_rows_ahead = false) {
+template <int G, class Rows>
+__device__ __forceinline__ void compete_over(Loaded<G>& in, const Dims& d, int group_index, const UnitPool& p,
+                                             const Rows& rows, uint8_t* sel, uint8_t* sel_lds, int tid,
+                                             const unsigned char* staged_k = nullptr, const unsigned char* staged_v = nullptr,
+                                             int staged_pitch = 0, bool pool_rows_ahead = false) {
   __shared__ uint4 s_pool_k[kPoolRowsAhead][16], s_pool_v[kPoolRowsAhead][16];
   __shared__ double c_score[kMaxCand];
   __shared__ int32_t c_idx[kMaxCand];
@@ -236,8 +250,8 @@ __device__ __forceinline__ void compete(Loaded<G>& in, const Dims& d, int group_
         mk[q] = *(const uint4*)(staged_k + (-src - 1) * staged_pitch + sub * 16);
         mvv[q] = *(const uint4*)(staged_v + (-src - 1) * staged_pitch + sub * 16);
       } else {
-        const __half* rk = src >= 0 ? p.pk + (int64_t)src * kHeadDim : gk + (int64_t)(-src - 1) * kHeadDim;
-        const __half* rv = src >= 0 ? p.pv + (int64_t)src * kHeadDim : gv + (int64_t)(-src - 1) * kHeadDim;
+        const __half* rk = src >= 0 ? p.pk + (int64_t)src * kHeadDim : rows.k(-src - 1);
+        const __half* rv = src >= 0 ? p.pv + (int64_t)src * kHeadDim : rows.v(-src - 1);
         mk[q] = *(const uint4*)(rk + sub * 8);
         mvv[q] = *(const uint4*)(rv + sub * 8);
       }
@@ -267,6 +281,15 @@ __device__ __forceinline__ void compete(Loaded<G>& in, const Dims& d, int group_
     *p.pool_count = n_old - n_ev + n_new;
     *p.aux_count = n_aux + n_ev;
   }
+}
+
+template <int G>
+__device__ __forceinline__ void compete(Loaded<G>& in, const Dims& d, int group_index, const UnitPool& p,
+                                        const __half* gk, const __half* gv, uint8_t* sel, uint8_t* sel_lds, int tid,
+                                        const unsigned char* staged_k = nullptr, const unsigned char* staged_v = nullptr,
+                                        int staged_pitch = 0, bool pool_rows_ahead = false) {
+  compete_over<G>(in, d, group_index, p, GroupOf{gk, gv}, sel, sel_lds, tid, staged_k, staged_v, staged_pitch,
+                  pool_rows_ahead);
 }
 
 }  // namespace trace_core

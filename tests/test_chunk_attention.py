@@ -1,0 +1,299 @@
+"""The attention of a chunk of new tokens over a cache and itself (kvq_prompt_attention) against 64 bits."""
+import numpy as np
+import pytest
+
+import kvq_synth as S
+from paper_2505_10938_amd import binding as B
+from paper_2505_10938_amd import cache as KC
+from tests import chunk_helpers as H
+
+pytestmark = pytest.mark.gpu
+
+PAPER = dict(bits=2, group_k=128, group_v=128, residual=32, outlier_budget=3, aux_capacity=32)
+
+
+def queries(total, heads, scale, seed):
+    g = np.random.default_rng(seed)
+    return (scale * g.standard_normal((total, heads, 128))).astype(np.float16)
+
+
+def filled(cfg, hist, K, V, paged=False):
+    """A cache of sequences with their first hist[b] tokens, by the calls that quantize prompts."""
+    import torch
+    pages = cfg.batch * (cfg.max_seq // cfg.group_k)
+    cache = KC.RaggedKVCache(cfg, n_pages=pages + 7 if paged else None)
+    if paged:
+        deal = np.random.default_rng(3).permutation(pages + 7)[:pages].reshape(cfg.batch, -1)
+        cache.page_table.copy_(torch.from_numpy(deal.astype(np.int32)))
+    for b, n in enumerate(hist):
+        if n:
+            k, v = (torch.from_numpy(np.ascontiguousarray(x[b][:, :n])).cuda() for x in (K, V))
+            cache.prefill_sequence(b, [k], [v])
+    return cache
+
+
+def check(out, cfg, hist, new, K, V, q, cross=False, sequences=None, heads=None):
+    """`out` [total, q_heads, 128] against the oracle, unit by unit."""
+    g = cfg.q_heads // cfg.kv_heads
+    out = out.cpu().numpy().astype(np.float64)
+    worst = at = 0
+    for b, n in enumerate(new):
+        for h in range(cfg.kv_heads):
+            if n == 0 or (sequences is not None and b not in sequences) or (heads is not None and h not in heads):
+                continue
+            st, k_ring, v_ring = H.state_of(cfg, K[b][h, :hist[b]], V[b][h, :hist[b]])
+            k, v = st.effective_rows(k_ring, v_ring)
+            exact = np.ones(len(k), bool)
+            exact[:st.n_quant] = st.masked
+            own = None
+            if not cross:
+                own, rows = len(k), slice(hist[b], hist[b] + n)
+                k, v = np.concatenate([k, K[b][h, rows]]), np.concatenate([v, V[b][h, rows]])
+                exact = np.concatenate([exact, np.ones(n, bool)])
+            mine = slice(h * g, (h + 1) * g)
+            want, allowed = H.attention(q[at:at + n, mine], k, v, own, exact)
+            err = np.abs(out[at:at + n, mine] - want)
+            assert np.isfinite(out[at:at + n, mine]).all(), (b, h)
+            assert (err <= allowed).all(), (b, h, float((err / np.maximum(allowed, 1e-30)).max()))
+            worst = max(worst, float((err / np.maximum(allowed, 1e-30)).max()))
+        at += n
+    return worst
+
+
+def run(cfg, hist, new, paged=False, cross=False, scale=1.0, seed=0, cache=None, **which):
+    import torch
+    K, V = H.rows_of(cfg, [a + n for a, n in zip(hist, new)], seed=seed)
+    cache = cache or filled(cfg, hist, K, V, paged)
+    q = queries(sum(new), cfg.q_heads, scale, seed + 1)
+    starts = torch.tensor(np.concatenate([[0], np.cumsum(new)]), dtype=torch.int32, device="cuda")
+    args = [None, None] if cross else [torch.from_numpy(np.concatenate(
+        [x[b][:, hist[b]:].transpose(1, 0, 2) for b in range(cfg.batch)])).cuda().contiguous() for x in (K, V)]
+    out = cache.attend(0, torch.from_numpy(q).cuda(), starts, max(new), *args)
+    return check(out, cfg, hist, new, K, V, q, cross, **which)
+
+
+@pytest.mark.parametrize("q_heads,kv_heads", [(2, 2), (4, 2), (8, 2), (8, 1)])
+@pytest.mark.parametrize("tokens,history", [(1, 0), (1, 1), (1, 700), (3, 159), (3, 160), (31, 161), (32, 500), (33, 0),
+                                            (64, 64), (65, 129), (127, 1000), (130, 333), (200, 0)])
+def test_chunks_of_all_lengths(q_heads, kv_heads, tokens, history):
+    cfg = H.config(1, 2, q_heads, kv_heads, 1024)
+    run(cfg, [history] * 2, [tokens] * 2, scale=0.3)
+
+
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("group_k,group_v", [(32, 32), (64, 64), (128, 128), (32, 128), (128, 32), (64, 32)])
+@pytest.mark.parametrize("paged", [False, True])
+def test_codes_of_all_settings(bits, group_k, group_v, paged):
+    cfg = H.config(1, 3, 8, 2, 1024, bits=bits, group_k=group_k, group_v=group_v)
+    run(cfg, [group_k * 5 + 150, 0, 3 * group_k + 131], [70, 40, 33], paged, scale=0.2)
+
+
+@pytest.mark.parametrize("kw", [dict(residual=0), dict(residual=37), dict(outlier_budget=0), dict(outlier_budget=40, aux_capacity=64),
+                                dict(outlier_budget=8, aux_capacity=0), dict(outlier_budget=0, aux_capacity=0), PAPER])
+def test_rings_and_pools_of_all_sizes(kw):
+    cfg = H.config(1, 2, 4, 2, 1024, **kw)
+    run(cfg, [700, 431], [50, 90], scale=0.2)
+
+
+def test_lengths_that_differ_and_sequences_without_tokens():
+    cfg = H.config(1, 6, 8, 2, 2048)
+    hist, new = [0, 1800, 5, 777, 0, 161], [1, 0, 129, 300, 64, 2]
+    run(cfg, hist, new, scale=0.2)
+    run(cfg, hist, new, paged=True, scale=0.2)
+
+
+def test_peaky_scores():
+    cfg = H.config(1, 2, 8, 2, 1024)
+    run(cfg, [600, 300], [40, 100], scale=1.0)
+
+
+@pytest.mark.parametrize("tokens", [1, 5, 100])
+def test_few_rows_over_a_long_cache(tokens):
+    """One unit's keys go to many workgroups, whose shares are put together."""
+    cfg = H.config(1, 1, 4, 1, 16384)
+    assert B.kvq_prompt_workspace_bytes(cfg, tokens, 15872, 159) > 0
+    run(cfg, [16000], [tokens], scale=0.1)
+
+
+@pytest.mark.parametrize("batch,tokens", [(70, 200), (3, 4000)])
+def test_enough_rows_for_one_workgroup_each(batch, tokens):
+    cfg = H.config(1, batch, 8, 2, 256) if batch > 3 else H.config(1, batch, 16, 8, 256)
+    assert B.kvq_prompt_workspace_bytes(cfg, tokens, 0, 159) == 0
+    run(cfg, [150] * batch, [tokens] * batch, scale=0.2, sequences=[0, batch - 1], heads=[0, cfg.kv_heads - 1])
+
+
+@pytest.mark.parametrize("history", [0, 77, 900])
+def test_queries_without_new_tokens_see_the_whole_cache(history):
+    cfg = H.config(1, 3, 8, 2, 1024)
+    run(cfg, [history, 0, 300], [37, 5, 130], cross=True, scale=0.3)
+
+
+def test_a_query_that_sees_nothing_gets_zeros():
+    import torch
+    cfg = H.config(1, 2, 8, 2, 1024)
+    cache = KC.KVCache(cfg)
+    out = cache.attend(0, torch.ones(2, 5, 8, 128, dtype=torch.float16, device="cuda"),
+                       out=torch.full((2, 5, 8, 128), float("nan"), dtype=torch.float16, device="cuda"))
+    assert torch.equal(out, torch.zeros_like(out))
+
+
+def test_one_length_for_all_equals_lengths_on_the_device():
+    import torch
+    cfg = H.config(1, 3, 8, 2, 1024)
+    K, V = H.rows_of(cfg, [500] * 3)
+    plain, ragged = KC.KVCache(cfg), filled(cfg, [430] * 3, K, V)
+    k, v = (torch.from_numpy(np.stack(x)).cuda() for x in (K, V))
+    plain.prefill(0, k[:, :, :430].contiguous(), v[:, :, :430].contiguous())
+    q = torch.from_numpy(queries(3 * 70, 8, 0.3, 1)).cuda()
+    # (Keys and Values of a token apart from the next one's, as parts of one projection's output)
+    wide = torch.empty(3 * 70, 12, 128, dtype=torch.float16, device="cuda")
+    wide[:, :8], wide[:, 8:10], wide[:, 10:] = q, k[:, :, 430:].transpose(1, 2).flatten(0, 1), v[:, :, 430:].transpose(1, 2).flatten(0, 1)
+    starts = torch.arange(0, 211, 70, dtype=torch.int32, device="cuda")
+    a = ragged.attend(0, wide[:, :8], starts, 70, wide[:, 8:10], wide[:, 10:])
+    b = plain.attend(0, wide[:, :8].unflatten(0, (3, 70)), wide[:, 8:10].unflatten(0, (3, 70)), wide[:, 10:].unflatten(0, (3, 70)))
+    c = plain.attend(0, q.view(3, 70, 8, 128), wide[:, 8:10].contiguous().view(3, 70, 2, 128), wide[:, 10:].contiguous().view(3, 70, 2, 128))
+    assert torch.equal(a, b.flatten(0, 1)) and torch.equal(b, c)
+
+
+def test_a_chunk_of_one_is_a_decode_step():
+    import torch
+    cfg = H.config(1, 4, 8, 2, 1024)
+    K, V = H.rows_of(cfg, [621] * 4)
+    k, v = (torch.from_numpy(np.stack(x)).cuda() for x in (K, V))
+    cache = KC.KVCache(cfg)
+    cache.prefill(0, k[:, :, :620].contiguous(), v[:, :, :620].contiguous())
+    q = torch.from_numpy(queries(4, 8, 0.2, 5)).cuda()
+    last = [x[:, :, 620].contiguous() for x in (k, v)]
+    chunk = cache.attend(0, q.view(4, 1, 8, 128), last[0].view(4, 1, 2, 128), last[1].view(4, 1, 2, 128))
+    step = cache.step(0, last[0], last[1], q)
+    again = cache.attend(0, q.view(4, 1, 8, 128))                     # the token is in the cache now
+    # both are held to 2e-3 of the exact result where the decode step is; the allowance of the chunk's own check is wider
+    assert (chunk[:, 0].float() - step.float()).abs().max() < 4e-3
+    assert (again[:, 0].float() - step.float()).abs().max() < 4e-3
+
+
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("tokens,bad", [(20, 7), (150, 64), (150, 149), (64, 0)])
+def test_new_tokens_behind_a_query_do_not_change_it(what, tokens, bad):
+    import torch
+    cfg = H.config(1, 1, 4, 2, 1024)
+    K, V = H.rows_of(cfg, [300 + tokens])
+    cache = filled(cfg, [300], K, V)
+    q = torch.from_numpy(queries(tokens, 4, 0.3, 2)).cuda()
+    k, v = (torch.from_numpy(x[0][:, 300:].transpose(1, 0, 2).copy()).cuda() for x in (K, V))
+    starts = torch.tensor([0, tokens], dtype=torch.int32, device="cuda")
+    want = cache.attend(0, q, starts, tokens, k, v)
+    for which in (0, 1, 2):
+        kk, vv = k.clone(), v.clone()
+        if which != 1:
+            kk[bad, :, 3] = what
+        if which != 0:
+            vv[bad, 0, 5] = what
+        got = cache.attend(0, q, starts, tokens, kk, vv)
+        assert torch.equal(got[:bad], want[:bad])
+        if which == 1:                                     # the Value: one channel of one kv head, of those that see it
+            rest = got.clone()
+            rest[bad:, :2, 5] = want[bad:, :2, 5]
+            assert torch.equal(rest, want)
+            assert not torch.isfinite(got[bad, :2, 5]).any()
+
+
+def test_what_holds_no_token_may_hold_anything():
+    import torch
+    cfg = H.config(1, 2, 8, 2, 1024, outlier_budget=8, aux_capacity=32)
+    K, V = H.rows_of(cfg, [740] * 2)
+    cache = filled(cfg, [700] * 2, K, V)
+    q = torch.from_numpy(queries(80, 8, 0.3, 2)).cuda()
+    k, v = (torch.from_numpy(np.concatenate([x[b][:, 700:].transpose(1, 0, 2) for b in (0, 1)])).cuda().contiguous() for x in (K, V))
+    starts = torch.tensor([0, 40, 80], dtype=torch.int32, device="cuda")
+    want = cache.attend(0, q, starts, 40, k, v)
+    slots = cache.sizes.pool_slots
+    live = cache.seq_state[0].tolist()
+    row = (torch.arange(cache.sizes.res_rows, device="cuda") - live[1]) % cache.sizes.res_rows >= live[2]
+    for name in ("k", "v"):
+        cache.res_view(name)[:, row] = float("nan")
+        pool = getattr(cache, "pool_" + name).view(torch.float16)[:cache.sizes.units * slots * 128].view(-1, slots, 128)
+        for u in range(cache.sizes.units):
+            n_in, n_aux = (int(t.view(torch.int32)[u]) for t in (cache.pool_count, cache.aux_count))
+            pool[u, n_in:8] = float("nan")
+            pool[u, 8 + n_aux:] = float("inf")
+    assert torch.equal(cache.attend(0, q, starts, 40, k, v), want)
+
+
+def test_rows_of_no_sequence_are_left_as_they_are():
+    import torch
+    cfg = H.config(1, 2, 8, 2, 1024)
+    cache = KC.RaggedKVCache(cfg)
+    q = torch.randn(50, 8, 128, device="cuda").half()
+    kv = torch.randn(50, 2, 128, device="cuda").half()
+    q[20:23] = kv[20:23] = float("nan")
+    q[41:] = kv[41:] = float("nan")
+    out = torch.full_like(q, 7.0)
+    # the starts are a row apart only where the array says so: a bound on the tokens below a sequence's cuts it short
+    cache.attend(0, q, torch.tensor([3, 23, 41], dtype=torch.int32, device="cuda"), 17, kv, kv, out=out)
+    assert (out[:3] == 7).all() and (out[20:23] == 7).all() and (out[40:] == 7).all()
+    assert torch.isfinite(out).all() and not (out[3:20] == 7).all()
+
+
+def test_starts_and_states_out_of_range_stay_inside():
+    import torch
+    cfg = H.config(1, 3, 8, 2, 1024)
+    K, V = H.rows_of(cfg, [400] * 3)
+    cache = filled(cfg, [400] * 3, K, V)
+    q, kv = torch.randn(60, 8, 128, device="cuda").half(), torch.randn(60, 2, 128, device="cuda").half()
+    good = cache.attend(0, q, torch.tensor([0, 20, 40, 60], dtype=torch.int32, device="cuda"), 20, kv, kv)
+    for starts in ([0, -5, 1 << 30, 60], [60, 40, 20, 0], [-(1 << 31), (1 << 31) - 1, 0, 60]):
+        cache.attend(0, q, torch.tensor(starts, dtype=torch.int32, device="cuda"), 20, kv, kv)
+    cache.seq_state[1] = torch.tensor([1 << 30, -7, 1 << 30, 1], dtype=torch.int32)
+    cache.seq_state[2] = torch.tensor([-64, 1 << 30, -1, 1], dtype=torch.int32)
+    got = cache.attend(0, q, torch.tensor([0, 20, 40, 60], dtype=torch.int32, device="cuda"), 20, kv, kv)
+    assert torch.equal(got[:20], good[:20])
+
+
+def test_calls_on_two_streams_and_in_two_graphs():
+    """Split launches: every call has a workspace of its own, so neither streams nor graphs meet in one."""
+    import torch
+    cfg = H.config(1, 1, 4, 1, 8192)
+    K, V = H.rows_of(cfg, [8000])
+    cache = filled(cfg, [7900], K, V)
+    assert B.kvq_prompt_workspace_bytes(cfg, 9, *cache.bounds()) > 0
+    inputs = []
+    for seed in (1, 2):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        inputs.append([torch.randn(9, heads, 128, generator=g, device="cuda").half() for heads in (4, 1, 1)])
+    starts = torch.tensor([0, 9], dtype=torch.int32, device="cuda")
+    want = [cache.attend(0, q, starts, 9, k, v) for q, k, v in inputs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in inputs]
+    outs = [torch.empty_like(w) for w in want]
+    for _ in range(20):
+        for s, o, (q, k, v) in zip(streams, outs, inputs):
+            cache.attend(0, q, starts, 9, k, v, out=o, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w) for o, w in zip(outs, want))
+    graphs = [torch.cuda.CUDAGraph() for _ in inputs]
+    for graph, o, (q, k, v) in zip(graphs, outs, inputs):
+        with torch.cuda.graph(graph):
+            cache.attend(0, q, starts, 9, k, v, out=o)
+    for turn in range(4):
+        for o in outs:
+            o.zero_()
+        torch.cuda.synchronize()
+        for s, graph in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(o, w) for o, w in zip(outs, want)), turn
+        eager = cache.attend(0, *[inputs[0][0], starts, 9, inputs[0][1], inputs[0][2]])
+        assert torch.equal(eager, want[0])
+
+
+def test_results_do_not_depend_on_the_run():
+    import torch
+    cfg = H.config(1, 2, 8, 2, 2048)
+    K, V = H.rows_of(cfg, [1500] * 2)
+    cache = filled(cfg, [1400] * 2, K, V)
+    q, kv = torch.randn(200, 8, 128, device="cuda").half(), torch.randn(200, 2, 128, device="cuda").half()
+    starts = torch.tensor([0, 100, 200], dtype=torch.int32, device="cuda")
+    first = cache.attend(0, q, starts, 100, kv, kv)
+    assert all(torch.equal(cache.attend(0, q, starts, 100, kv, kv), first) for _ in range(5))
