@@ -909,9 +909,11 @@ int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q
   if (((uintptr_t)qc.mask) & 3) return KVQ_ERR_INVALID_ARG;
   const int64_t g = cfg->q_heads / cfg->kv_heads;
   const ChunkShape shape = chunk_shape(cfg, chunk.max_tokens, n_quant, n_res, k_new != nullptr);
-  const int64_t items = (int64_t)cfg->batch * cfg->kv_heads * shape.row_tiles * shape.splits;
+  const int64_t units = (int64_t)cfg->batch * cfg->kv_heads, items = units * shape.row_tiles * shape.splits;
+  int32_t parts = 1;
+  while (units * parts % 8) parts *= 2;
   // (rows and the keys of a tile are numbered in 32 bits; a launch has less than 2^32 threads)
-  if (chunk.max_tokens * g > (1 << 30) || items > (1 << 24) - 16) return KVQ_ERR_UNSUPPORTED;
+  if (chunk.max_tokens * g > (1 << 30) || items > (1 << 23)) return KVQ_ERR_UNSUPPORTED;
   const int64_t need = chunk_workspace_bytes(cfg, shape);
   if (need > 0 && (!workspace || (((uintptr_t)workspace) & 255) || (int64_t)workspace_bytes < need)) return KVQ_ERR_WORKSPACE;
 
@@ -945,7 +947,8 @@ int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q
   a.scale = 0.08838834764831845f * 1.4426950408889634f;
   a.row_tiles = (int32_t)shape.row_tiles;
   a.splits = (int32_t)shape.splits;
-  a.items = (uint32_t)items;
+  a.parts = parts;
+  a.part_tiles = (int32_t)((shape.row_tiles + parts - 1) / parts);
   const int64_t shares = items * kvq::kChunkRows;
   a.share_o = (float*)workspace;
   a.share_ml = need > 0 ? a.share_o + shares * cfg->head_dim : nullptr;

@@ -163,7 +163,8 @@ struct ChunkArgs {
   float scale;                          // 1 / sqrt(head_dim) * log2(e): scores are kept in powers of two
   int32_t row_tiles;                    // workgroups per unit along the query rows, of max_tokens tokens
   int32_t splits;                       // workgroups that share a row tile's keys
-  uint32_t items;                       // units * row_tiles * splits
+  int32_t parts;                        // 1, 2, 4 or 8: units * parts is a multiple of 8
+  int32_t part_tiles;                   // row tiles of a part of a unit: row_tiles / parts, rounded up
   float* share_ml;                      // splits > 1: [unit][row][split][2] maximum (log2) and sum of a row's share
   float* share_o;                       //             [unit][row][split][head_dim]
 };

@@ -98,15 +98,15 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 
   // ---- which rows, which keys
-  // Workgroups go round the eight XCDs; each takes a run of neighbouring work items, so that those that share a unit's
-  // keys share an L2 cache as well.
-  const uint32_t per_xcd = gridDim.x >> 3;
-  const uint32_t item = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
-  if (item >= a.items) return;
-  const uint32_t per_unit = a.row_tiles * a.splits;
-  const int ul = item / per_unit;
-  const uint32_t in_unit = item - ul * per_unit;
-  const int tile_back = in_unit / a.splits, split = in_unit - tile_back * a.splits;
+  // Workgroups go round the eight XCDs.  An XCD takes whole units (where their number is no multiple of eight, every
+  // `parts`-th row tile of them), unit after unit, so that those that share a unit's keys share an L2 cache as well, and
+  // sequences of different lengths weigh on all XCDs alike.
+  const uint32_t per_unit = a.part_tiles * a.splits, turn = blockIdx.x >> 3;
+  const uint32_t at = turn / per_unit, in_unit = turn - at * per_unit;
+  const uint32_t part_unit = 8 * at + (blockIdx.x & 7);
+  const int ul = part_unit / a.parts;
+  const int tile_in_part = in_unit / a.splits, split = in_unit - tile_in_part * a.splits;
+  const int tile_back = tile_in_part * a.parts + (part_unit - ul * a.parts);
   const int b = ul / d.kv_heads, h = ul - b * d.kv_heads;
   const ChunkRows mine = chunk_rows(a.starts, a.total, a.max_tokens, b);
   const int64_t s0 = mine.first;
@@ -245,13 +245,24 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
     const int r = lane >> 4, m16 = lane & 15;
     QuantRegs<BITS, NV> R;
     uint32_t mask0 = 0, mask1 = 0;
-    auto place = [&](int blk) {                          // (one block behind the last: the last one again, all of it hidden)
-      const GroupPlace at = place_of_group(d, ul, blk >> d.bpg_shift);
-      return at;
+    // The page numbers of 64 groups at a time, a lane each: a look into the table for every tile would have the tile's loads
+    // wait for it.
+    int pages = 0, first_group = -64;
+    auto place = [&](int blk) -> GroupPlace {            // (called with ascending blocks, but for those of one tile)
+      const int group = blk >> d.bpg_shift;
+      if (!d.page_table) return {u, group};
+      if (group - first_group >= 64) {                   // uniform
+        first_group = group;
+        pages = d.page_table[(int64_t)b * d.table_stride + min(group + lane, last >> d.bpg_shift)];
+      }
+      const int page = __builtin_amdgcn_readlane(pages, group - first_group);
+      return {d.plane0 + h, min(max(page, 0), d.n_pages - 1)};
     };
     auto load = [&](int tile) {
-      const int blk = min(2 * tile + (wave & 1), last);
-      const GroupPlace at = place(blk);
+      const int b0 = 2 * tile, b1 = min(2 * tile + 1, last);     // (behind the last block: that one again, all of it hidden)
+      const GroupPlace g0 = place(b0), g1 = place(b1);
+      const int blk = (wave & 1) ? b1 : b0;
+      const GroupPlace at = (wave & 1) ? g1 : g0;
       const int64_t pblk = at.row * d.blocks_per_unit + ((int64_t)at.slot << d.bpg_shift) + (blk & ((1 << d.bpg_shift) - 1));
       const u32x4* codes = (const u32x4*)((which ? a.v_codes : a.k_codes) + pblk * d.block_bytes);
 #pragma unroll
@@ -272,8 +283,6 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
         }
       }
       // (every wavefront wants both blocks' mask words)
-      const int b0 = 2 * tile, b1 = min(2 * tile + 1, last);
-      const GroupPlace g0 = place(b0), g1 = place(b1);
       const int in_group = (1 << d.bpg_shift) - 1;
       mask0 = a.mask[g0.row * d.blocks_per_unit + ((int64_t)g0.slot << d.bpg_shift) + (b0 & in_group)];
       mask1 = a.mask[g1.row * d.blocks_per_unit + ((int64_t)g1.slot << d.bpg_shift) + (b1 & in_group)];
@@ -518,7 +527,8 @@ __global__ void __launch_bounds__(kThreads) prompt_merge_kernel(ChunkArgs a) {
 }  // namespace
 
 hipError_t launch_prompt_attention(const ChunkArgs& a, hipStream_t s) {
-  const uint32_t grid = (a.items + 7) / 8 * 8;
+  const int64_t units = (int64_t)a.d.units_per_layer * a.parts;
+  const uint32_t grid = (uint32_t)(units * a.part_tiles * a.splits);
   auto go = [&](auto kern) {
     hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kBytesBuffer);
     if (e != hipSuccess) return e;
