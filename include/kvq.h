@@ -551,7 +551,7 @@ typedef struct kvq_chunk {
  *   q          : device fp16, token i of the packed array at element offset i * q_stride, its q_heads rows of head_dim
  *                behind each other; 16-byte aligned; q_stride >= q_heads * head_dim, a multiple of 8
  *   k_new, v_new : device fp16, token i's kv_heads rows at element offset i * kv_stride; 16-byte aligned; kv_stride >=
- *                kv_heads * head_dim, a multiple of 8.  (q, k_new and v_new may be parts of one projection's output.)
+ *                kv_heads * head_dim, a multiple of 8, at most 2^23 (as q_stride).  (q, k_new and v_new may be parts of one projection's output.)
  *                Both NULL: no new tokens, every query sees the whole cache and nothing else (cross attention to an
  *                encoder's states); kv_stride is ignored
  *   seq_state  : as in kvq_decode_attention_ragged, with n_quant and n_res upper bounds of the sequences' (longer ones

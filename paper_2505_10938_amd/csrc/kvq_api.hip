@@ -843,8 +843,9 @@ int32_t check_chunk(const kvq_config* cfg, const kvq_chunk& c) {
   if (!c.starts && (int64_t)cfg->batch * c.max_tokens != c.total) return KVQ_ERR_INVALID_ARG;
   return KVQ_OK;
 }
+// (strides are at most 2^23 elements: 64 tokens are less than 2^30 bytes apart)
 bool rows_ok(const void* p, int64_t stride, int64_t heads, int64_t head_dim) {
-  return p && (((uintptr_t)p) & 15) == 0 && stride >= heads * head_dim && stride % 8 == 0;
+  return p && stride <= (1 << 23) && (((uintptr_t)p) & 15) == 0 && stride >= heads * head_dim && stride % 8 == 0;
 }
 
 // How a chunk's attention is dealt: row tiles of a unit, and workgroups that share a row tile's keys where the row tiles

@@ -14,6 +14,7 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef __fp16 lds_half4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) lds_half4* lds_half4_ptr;
 typedef float float16v __attribute__((ext_vector_type(16)));
+typedef float float2v __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
@@ -69,9 +70,9 @@ __device__ __forceinline__ u32x4 dequant_field(const uint32_t (&w)[2 * BITS], in
   return r;
 }
 
-__device__ __forceinline__ uint32_t not_finite(uint32_t w) {      // either half an infinity or a NaN
-  return ((w & 0x7C00u) == 0x7C00u) | ((w & 0x7C000000u) == 0x7C000000u);
-}
+// The larger of two numbers, or a NaN (one instruction for three: of what comes out of a matrix instruction the ordinary
+// maximum has every operand made canonical first).
+__device__ __forceinline__ float largest(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 // The value of lane ^ 32.
 __device__ __forceinline__ float other_half(float v) {
@@ -129,8 +130,11 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
   const int live_rows = (int)min((int64_t)kRows, (int64_t)n * d.g - first_row);
   const int first_token = first_row >> a.g_shift;
   const int n_new = a.k_new ? min(n, ((first_row + live_rows - 1) >> a.g_shift) + 1) : 0;
-  const int tq = (nq + kTile - 1) / kTile, tr = (n_rows + kTile - 1) / kTile, tn = (n_new + kTile - 1) / kTile;
-  const int tiles = tq + tr + tn;
+  // Tiles, in this order: quantized tokens; new tokens that every row of the workgroup sees; full-precision rows of the
+  // cache; the other new tokens.
+  const int tq = (nq + kTile - 1) / kTile, tr = (n_rows + kTile - 1) / kTile;
+  const int ti = a.k_new ? min(n, first_token + 1) / kTile : 0, tn = (n_new + kTile - 1) / kTile - ti;
+  const int tiles = tq + ti + tr + tn;
   const int per = (tiles + a.splits - 1) / a.splits;
   const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
 
@@ -159,43 +163,53 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
   unsigned char* buffer = smem;
   auto other = [&](unsigned char* p) { return smem + (p == smem ? kBytesBuffer : 0); };
 
-  // First product, softmax, second product of one tile.  `limit`: keys of the tile below it are seen by the lane's row;
-  // `hidden`: blocks' mask words (quantized tiles).  V stands as rows of channels (two transposing reads bring four keys each of a channel to
-  // a lane) or, dequantized, already by channel in the order of the second product.
-  auto compute = [&](auto quantized, const unsigned char* buf, int limit, bool all, uint32_t hidden0, uint32_t hidden1,
-                     float (&p)[2][16]) {
+  // First product, softmax, second product of one tile.  V stands as rows of channels (two transposing reads bring four keys
+  // each of a channel to a lane) or, dequantized, already by channel in the order of the second product.  `hide(x)` sets the
+  // scores of keys that a row does not see to -infinity, `keep(p)` may look at the weights.
+  auto compute = [&](auto quantized, const unsigned char* buf, auto hide, auto keep) {
     constexpr bool QUANT = decltype(quantized)::value;
     const unsigned char* sk = buf + col * kPitchK + 16 * half;
+    const unsigned char* sv = buf + kBytesK;
+    auto value = [&](int s, int c) -> half8 {
+      if (QUANT) return *(const half8*)(sv + (32 * c + col) * kPitchT + 32 * s + 16 * half);
+      const unsigned char* at = sv + (16 * s + 4 * half + ((lane & 15) >> 2)) * kPitchV + 2 * (32 * c + (lane & 16) + 4 * (lane & 3));
+      const half4 lo = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_half4_ptr)at));
+      const half4 hi = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_half4_ptr)(at + 8 * kPitchV)));
+      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    // A compute unit has two workgroups, a SIMD a wavefront of each.  The one that has matrix instructions to issue goes first,
+    // so that the other's softmax fills the gaps (8192 tokens, 32 heads: 668 us with no or 695 with the other order, 641 so).
+    // (Eight operands on their way ahead of the matrix instructions, and the first four of the second product's: left to
+    // itself the compiler asks for two at a time and waits for them.)
     float16v x[2];
+    half8 k[16], v0[4];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int r = 0; r < 16; ++r) x[0][r] = x[1][r] = 0.0f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[t][r] = 0.0f;
+    for (int s = 0; s < 8; ++s)
 #pragma unroll
-      for (int s = 0; s < 8; ++s)
-        x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)(sk + 32 * t * kPitchK + 32 * s), q[s], x[t], 0, 0, 0);
+      for (int t = 0; t < 2; ++t) k[2 * s + t] = *(const half8*)(sk + 32 * t * kPitchK + 32 * s);
+#pragma unroll
+    for (int s = 0; s < 8; ++s)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[2 * s + t], q[s], x[t], 0, 0, 0);
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v0[c] = value(0, c);
+    __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
-    if (QUANT) {
-      if (hidden0 | hidden1) {                           // uniform
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, QUANT ? 4 : 8, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+    __builtin_amdgcn_s_setprio(0);
+    hide(x);
+    float top = largest(x[0][0], x[1][0]);
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          const uint32_t word = (t ? hidden1 : hidden0) >> (4 * half);
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            if (word & (1u << (8 * (r >> 2) + (r & 3)))) x[t][r] = -__builtin_inff();
-        }
-      }
-    } else if (!all) {                                   // uniform
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r)
-          if (32 * t + 8 * (r >> 2) + (r & 3) + 4 * half >= limit) x[t][r] = -__builtin_inff();
-    }
-    float top = fmaxf(x[0][0], x[1][0]);
-#pragma unroll
-    for (int r = 1; r < 16; ++r) top = fmaxf(top, fmaxf(x[0][r], x[1][r]));
-    top = fmaxf(top, other_half(top)) * a.scale;
+    for (int r = 1; r < 16; ++r) top = largest(largest(top, x[0][r]), x[1][r]);
+    top = largest(top, other_half(top)) * a.scale;
     if (__any(top > m + kSlack)) {
       const float m_new = fmaxf(m, top);
       const float down = __builtin_amdgcn_exp2f(m - m_new);
@@ -206,36 +220,28 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
 #pragma unroll
         for (int r = 0; r < 16; ++r) o[c][r] *= down;
     }
-    float sum = 0.0f;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        p[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], a.scale, -m));
-        sum += p[t][r];
-      }
-    l += sum;
-    const unsigned char* sv = buf + kBytesK;
+      for (int r = 0; r < 16; ++r) x[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], a.scale, -m));
+    keep(x);
+    __builtin_amdgcn_s_setprio(1);                       // (see above)
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      half8 w;
+      half2v w[4];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = (_Float16)p[s >> 1][8 * (s & 1) + j];
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        half8 v;
-        if (QUANT) {
-          v = *(const half8*)(sv + (32 * c + col) * kPitchT + 32 * s + 16 * half);
-        } else {
-          const unsigned char* at = sv + (16 * s + 4 * half + ((lane & 15) >> 2)) * kPitchV + 2 * (32 * c + (lane & 16) + 4 * (lane & 3));
-          const half4 lo = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_half4_ptr)at));
-          const half4 hi = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_half4_ptr)(at + 8 * kPitchV)));
-          v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
-        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(v, w, o[c], 0, 0, 0);
+      for (int j = 0; j < 4; ++j) {
+        const float2v pair = {x[s >> 1][8 * (s & 1) + 2 * j], x[s >> 1][8 * (s & 1) + 2 * j + 1]};
+        w[j] = __builtin_convertvector(pair, half2v);
+        l = __builtin_amdgcn_fdot2(w[j], half2v{1, 1}, l, false);       // (the sum of the weights as they are used)
       }
+      const half8 weights = {w[0][0], w[0][1], w[1][0], w[1][1], w[2][0], w[2][1], w[3][0], w[3][1]};
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s == 0 ? v0[c] : value(s, c), weights, o[c], 0, 0, 0);
     }
   };
+  const auto nothing = [](auto&) {};
 
   // ---- quantized tokens, 64 (two blocks) a tile: each wavefront turns one block's Keys or Values into fp16 rows
   {
@@ -331,8 +337,20 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
       for (int t = t_begin; t < qe; ++t) {
         const bool more = t + 1 < qe;
         if (more) load(t + 1);
-        float p[2][16];
-        if (wave_live) compute(std::true_type{}, buffer, kTile, true, __builtin_amdgcn_readfirstlane(h0), __builtin_amdgcn_readfirstlane(h1), p);
+        if (wave_live) {
+          const uint32_t hidden[2] = {(uint32_t)__builtin_amdgcn_readfirstlane(h0), (uint32_t)__builtin_amdgcn_readfirstlane(h1)};
+          compute(std::true_type{}, buffer, [&](float16v (&x)[2]) {
+            if (hidden[0] | hidden[1]) {                 // uniform
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const uint32_t word = hidden[i] >> (4 * half);
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                  if (word & (1u << (8 * (r >> 2) + (r & 3)))) x[i][r] = -__builtin_inff();
+              }
+            }
+          }, nothing);
+        }
         buffer = other(buffer);
         if (more) {
           h0 = mask0;
@@ -344,80 +362,100 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
     }
   }
 
-  // ---- full-precision rows, 64 a tile: the pools' members and the ring, then the new tokens
+  // ---- full-precision rows, 64 a tile
+  const int piece = tid & 15, line = tid >> 4;
+  u32x4 rk[4], rv[4];
+  auto store = [&](unsigned char* buf) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      *(u32x4*)(buf + (16 * i + line) * kPitchK + 16 * piece) = rk[i];
+      *(u32x4*)(buf + kBytesK + (16 * i + line) * kPitchV + 16 * piece) = rv[i];
+    }
+  };
+
+  // new tokens that all of the workgroup's rows see
   {
-    const int fb = max(t_begin, tq);
-    const int piece = tid & 15, line = tid >> 4;
-    u32x4 rk[4], rv[4];
+    const int nb = max(t_begin, tq), ne = min(t_end, tq + ti);
+    if (nb < ne) {
+      const uint32_t row_bytes = (uint32_t)a.kv_stride * 2, offset = line * row_bytes + 16 * piece;
+      const int64_t first = s0 * a.kv_stride + h * kHeadDim;
+      auto load = [&](int tile) {
+        const int64_t at = 2 * (first + (int64_t)(tile - tq) * kTile * a.kv_stride);       // (uniform)
+        const unsigned char* pk = (const unsigned char*)a.k_new + at;
+        const unsigned char* pv = (const unsigned char*)a.v_new + at;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          rk[i] = *(const u32x4*)(pk + (offset + 16 * i * row_bytes));
+          rv[i] = *(const u32x4*)(pv + (offset + 16 * i * row_bytes));
+        }
+      };
+      load(nb);
+      store(buffer);
+      __syncthreads();
+      for (int t = nb; t < ne; ++t) {
+        const bool more = t + 1 < ne;
+        if (more) load(t + 1);
+        if (wave_live) compute(std::false_type{}, buffer, nothing, nothing);
+        buffer = other(buffer);
+        if (more) store(buffer);
+        __syncthreads();
+      }
+    }
+  }
+
+  // the pools' members and the ring, then the new tokens that some of the rows do not see
+  {
+    const int fb = max(t_begin, tq + ti), rows_end = tq + ti + tr;
     const __half* pk = a.pool_k + u * d.pool_slots * kHeadDim + 8 * piece;
     const __half* pv = a.pool_v + u * d.pool_slots * kHeadDim + 8 * piece;
     const __half* ck = a.k_res + u * d.res_rows * kHeadDim + 8 * piece;
     const __half* cv = a.v_res + u * d.res_rows * kHeadDim + 8 * piece;
     const __half* nk = a.k_new + s0 * a.kv_stride + h * kHeadDim + 8 * piece;
     const __half* nv = a.v_new + s0 * a.kv_stride + h * kHeadDim + 8 * piece;
-    auto load = [&](int tile) {
-      const u32x4 none = {0, 0, 0, 0};
-      if (tile < tq + tr) {                              // uniform
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = (tile - tq) * kTile + 16 * i + line;
-          rk[i] = rv[i] = none;
-          if (e < n_rows) {
-            int at = e < n_pool ? e : d.pool_slots - d.A + (e - n_pool);
-            if (e >= n_pool + n_aux) {
-              at = rs + (e - n_pool - n_aux);
-              at -= at >= d.res_rows ? d.res_rows : 0;
-              rk[i] = *(const u32x4*)(ck + at * kHeadDim);
-              rv[i] = *(const u32x4*)(cv + at * kHeadDim);
-            } else {
-              rk[i] = *(const u32x4*)(pk + at * kHeadDim);
-              rv[i] = *(const u32x4*)(pv + at * kHeadDim);
-            }
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int e = (tile - tq - tr) * kTile + 16 * i + line;
-          rk[i] = rv[i] = none;
-          if (e < n_new) {
-            rk[i] = *(const u32x4*)(nk + e * a.kv_stride);
-            rv[i] = *(const u32x4*)(nv + e * a.kv_stride);
-          }
-        }
-      }
-    };
     // Where some rows see a new token and others do not, its Value must not reach the others, for 0 times an infinity is a
     // NaN: what is not finite is left out of the tile (and counted in by `late` for the rows that see it).
-    auto store = [&](unsigned char* buf, bool partly) {
-      uint32_t odd = 0;
+    auto load = [&](int tile) -> bool {
+      const bool own = tile >= rows_end;                 // uniform
+      const int first = own ? (tile - rows_end + ti) * kTile : (tile - tq - ti) * kTile;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (partly) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t bad = not_finite(rv[i][k]);
-            odd |= bad;
-            const uint32_t w = rv[i][k];
-            rv[i][k] = ((w & 0x7C00u) == 0x7C00u ? 0u : w & 0xFFFFu) | ((w & 0x7C000000u) == 0x7C000000u ? 0u : w & 0xFFFF0000u);
-          }
+        const int e = first + 16 * i + line;
+        rk[i] = rv[i] = u32x4{0, 0, 0, 0};
+        const __half* fk;
+        const __half* fv;
+        if (own) {
+          fk = nk + e * a.kv_stride;
+          fv = nv + e * a.kv_stride;
+        } else {
+          int at = rs + (e - n_pool - n_aux);
+          at -= at >= d.res_rows ? d.res_rows : 0;
+          const bool pooled = e < n_pool + n_aux;
+          if (pooled) at = e < n_pool ? e : d.pool_slots - d.A + (e - n_pool);
+          fk = (pooled ? pk : ck) + at * kHeadDim;
+          fv = (pooled ? pv : cv) + at * kHeadDim;
         }
-        *(u32x4*)(buf + (16 * i + line) * kPitchK + 16 * piece) = rk[i];
-        *(u32x4*)(buf + kBytesK + (16 * i + line) * kPitchV + 16 * piece) = rv[i];
+        if (e < (own ? n_new : n_rows)) {
+          rk[i] = *(const u32x4*)fk;
+          rv[i] = *(const u32x4*)fv;
+        }
       }
+      return own;
+    };
+    auto sort_out = [&]() {
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t w = rv[i][k], lo = (w & 0x7C00u) == 0x7C00u ? 0xFFFFu : 0u, hi = (w & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u;
+          odd |= lo | hi;
+          rv[i][k] = w & ~(lo | hi);
+        }
       return odd;
     };
-    auto seen_partly = [&](int tile) { return tile >= tq + tr && (tile - tq - tr + 1) * kTile - 1 > first_token; };
-    // The Values left out of a tile, for the rows that see them.  Weights go through LDS (the buffer that is not in use).
-    auto late = [&](int tile, int limit, unsigned char* spare, const float (&p)[2][16]) {
-      float* mine = (float*)(spare + wave * (kWaveRows * kTile * 4));
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mine[(32 * t + 8 * (r >> 2) + 4 * half + (r & 3)) * kWaveRows + col] = p[t][r];
-      __builtin_amdgcn_s_waitcnt(0xc07f);                // lgkmcnt(0): the wavefront's own stores
-      __builtin_amdgcn_wave_barrier();
-      const int base = (tile - tq - tr) * kTile;
+    // The Values left out of a tile, for the rows that see them.  Weights have gone through LDS (the buffer that is not in use).
+    auto late = [&](int tile, int limit, const float* mine) {
+      const int base = (tile - rows_end + ti) * kTile;
       for (int k = 0; k < kTile && base + k < n_new; ++k) {
         const float w = mine[k * kWaveRows + col];
         const __half* vr = a.v_new + (s0 + base + k) * a.kv_stride + h * kHeadDim + 4 * half;
@@ -433,29 +471,46 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
       }
     };
     if (fb < t_end) {
-      load(fb);
-      bool odd = __syncthreads_or(store(buffer, seen_partly(fb)));
+      bool odd = load(fb) && sort_out();
+      store(buffer);
+      odd = __syncthreads_or(odd);
       for (int t = fb; t < t_end; ++t) {
         const bool more = t + 1 < t_end;
-        if (more) load(t + 1);
-        // how many of the tile's keys the lane's row sees, and whether every row of the wavefront sees all
-        const bool own_new = t >= tq + tr;
-        const int base = own_new ? (t - tq - tr) * kTile : (t - tq) * kTile;
-        const int limit = (own_new ? min(n_new, token + 1) : n_rows) - base;
-        const int least = (own_new ? min(n_new, (wave_row >> a.g_shift) + 1) : n_rows) - base;
-        const int most = (own_new ? min(n_new, ((wave_row + kWaveRows - 1) >> a.g_shift) + 1) : n_rows) - base;
+        bool next_own = false;
+        if (more) next_own = load(t + 1);
+        // how many of the tile's keys the lane's row sees, and the most that a row of the wavefront does
+        const bool own = t >= rows_end;
+        const int base = own ? (t - rows_end + ti) * kTile : (t - tq - ti) * kTile;
+        const int limit = (own ? min(n_new, token + 1) : n_rows) - base;
+        const int most = (own ? min(n_new, ((wave_row + kWaveRows - 1) >> a.g_shift) + 1) : n_rows) - base;
         if (wave_live && most > 0) {
-          float p[2][16];
-          compute(std::false_type{}, buffer, limit, least >= kTile, 0u, 0u, p);
-          if (odd) late(t, limit, other(buffer), p);
+          float* mine = (float*)(other(buffer) + wave * (kWaveRows * kTile * 4));
+          compute(std::false_type{}, buffer, [&](float16v (&x)[2]) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+              for (int r = 0; r < 16; ++r)
+                if (32 * i + 8 * (r >> 2) + (r & 3) + 4 * half >= limit) x[i][r] = -__builtin_inff();
+          }, [&](float16v (&x)[2]) {
+            if (odd) {                                   // uniform
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mine[(32 * i + 8 * (r >> 2) + 4 * half + (r & 3)) * kWaveRows + col] = x[i][r];
+            }
+          });
+          if (odd) {
+            __builtin_amdgcn_s_waitcnt(0xc07f);          // lgkmcnt(0): the wavefront's own stores
+            __builtin_amdgcn_wave_barrier();
+            late(t, limit, mine);
+          }
         }
         buffer = other(buffer);
         if (more) {
-          const bool partly = seen_partly(t + 1);
           if (odd) __syncthreads();                      // (the weights' place in the other buffer)
-          const uint32_t found = store(buffer, partly);
-          if (partly) odd = __syncthreads_or(found);
-          else { __syncthreads(); odd = false; }
+          odd = next_own && sort_out();
+          store(buffer);
+          odd = __syncthreads_or(odd);
         }
       }
     }
