@@ -839,6 +839,7 @@ int32_t shift_of(int32_t power) { return power == 1 ? 0 : power == 2 ? 1 : power
 // The chunk's rows as the kernels take them, and where they are: token i of a packed array at element offset i * stride.
 int32_t check_chunk(const kvq_config* cfg, const kvq_chunk& c) {
   if (c.total < 1 || c.max_tokens < 1 || c.max_tokens > c.total) return KVQ_ERR_INVALID_ARG;
+  if (c.max_tokens > (1 << 30)) return KVQ_ERR_UNSUPPORTED;
   if (((uintptr_t)c.starts) & 3) return KVQ_ERR_INVALID_ARG;
   if (!c.starts && (int64_t)cfg->batch * c.max_tokens != c.total) return KVQ_ERR_INVALID_ARG;
   return KVQ_OK;
@@ -983,7 +984,7 @@ int32_t kvq_extend(const kvq_config* cfg, int32_t layer, const void* k_new, cons
     return KVQ_ERR_INVALID_ARG;
   if (!qcache_ok(cfg, qc) || !selected) return KVQ_ERR_INVALID_ARG;
   const int64_t units = (int64_t)cfg->batch * cfg->kv_heads, most = ((int64_t)chunk.max_tokens + G - 1) / G;
-  if (chunk.max_tokens > (1 << 30) || units * most > (1 << 22) - 1) return KVQ_ERR_UNSUPPORTED;   // (threads of a launch)
+  if (units * most > (1 << 22) - 1) return KVQ_ERR_UNSUPPORTED;   // (threads of a launch)
   if ((int64_t)selected_bytes < units * most * G) return KVQ_ERR_WORKSPACE;
   return from_hip(kvq::launch_extend(make_dims(cfg, layer, qc), (const __half*)k_new, (const __half*)v_new, kv_stride, chunk,
                                      res, seq_state, n_quant, res_start, n_res, pool, selected, qc, (hipStream_t)stream));

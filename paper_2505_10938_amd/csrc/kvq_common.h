@@ -231,6 +231,14 @@ hipError_t launch_rope(const __half* x, int64_t rows, int32_t rows_per_seq, cons
                        __half* out, hipStream_t s);
 int decode_wave_lds_bytes(int g, int vgroups);   // LDS one decode wavefront needs
 
+// Where a group's rows are: `k(t)`, `v(t)` of token t.  Behind each other:
+struct GroupOf {
+  const __half* gk;
+  const __half* gv;
+  __device__ __forceinline__ const __half* k(int t) const { return gk + t * kHeadDim; }
+  __device__ __forceinline__ const __half* v(int t) const { return gv + t * kHeadDim; }
+};
+
 // ---- exchanges inside a row of 16 lanes on the DPP path (no LDS traffic) -----------------------
 // Step s of a butterfly over 2, 4, 8, 16 adjacent lanes: the value of lane ^ 1, of lane ^ 2, then of
 // the mirror lane inside 8 and inside 16.  The mirrors pair a lane with one of the other half; they

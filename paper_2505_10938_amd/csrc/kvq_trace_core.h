@@ -57,14 +57,6 @@ __device__ inline UnitPool unit_pool(const Dims& d, int64_t u, __half* pool_k, _
   return p;
 }
 
-// Where a group's rows are: `k(t)`, `v(t)` of token t.  Behind each other:
-struct GroupOf {
-  const __half* gk;
-  const __half* gv;
-  __device__ __forceinline__ const __half* k(int t) const { return gk + t * kHeadDim; }
-  __device__ __forceinline__ const __half* v(int t) const { return gv + t * kHeadDim; }
-};
-
 // What the first phase loads.
 template <int G>
 struct Loaded {
