@@ -292,7 +292,6 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
       const int in_group = (1 << d.bpg_shift) - 1;
       mask0 = a.mask[g0.row * d.blocks_per_unit + ((int64_t)g0.slot << d.bpg_shift) + (b0 & in_group)];
       mask1 = a.mask[g1.row * d.blocks_per_unit + ((int64_t)g1.slot << d.bpg_shift) + (b1 & in_group)];
-      if (2 * tile + 1 > last) mask1 = ~0u;
     };
     auto store = [&](unsigned char* buf) {
       const int at = 32 * (wave & 1);                    // the block's tokens of the tile
@@ -330,8 +329,10 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
       }
     };
     if (t_begin < qe) {
+      // (the words are looked at when the tile is, not when they are asked for: everything would wait for them)
+      auto second = [&](int tile) { return 2 * tile + 1 > last ? ~0u : mask1; };
       load(t_begin);
-      uint32_t h0 = mask0, h1 = mask1;
+      uint32_t h0 = mask0, h1 = second(t_begin);
       store(buffer);
       __syncthreads();
       for (int t = t_begin; t < qe; ++t) {
@@ -353,9 +354,9 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
         }
         buffer = other(buffer);
         if (more) {
-          h0 = mask0;
-          h1 = mask1;
           store(buffer);
+          h0 = mask0;
+          h1 = second(t + 1);
         }
         __syncthreads();
       }
@@ -544,7 +545,8 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
       *(float4*)(to + 32 * c + 8 * r4) = make_float4(o[c][4 * r4], o[c][4 * r4 + 1], o[c][4 * r4 + 2], o[c][4 * r4 + 3]);
 }
 
-// The shares of a row's splits put together: sum of 2^(m_i - max m) (l_i, o_i).  32 lanes a row.
+// The shares of a row's splits put together: sum of 2^(m_i - max m) (l_i, o_i).  32 lanes a row: a lane has the maximum and the
+// sum of one of 32 splits, and four channels; the splits' rows are asked for eight at a time.
 __global__ void __launch_bounds__(kThreads) prompt_merge_kernel(ChunkArgs a) {
   const Dims& d = a.d;
   const int sub = threadIdx.x & 31;
@@ -555,21 +557,42 @@ __global__ void __launch_bounds__(kThreads) prompt_merge_kernel(ChunkArgs a) {
   const int n = mine.n;
   if (row >= (int64_t)n * d.g) return;
   const int64_t place = ((int64_t)ul * a.row_tiles * kRows + row) * a.splits;
-  const float* ml = a.share_ml + 2 * place;
-  float m = kNegBig;
-  for (int i = 0; i < a.splits; ++i)
-    if (ml[2 * i + 1] != 0.0f) m = fmaxf(m, ml[2 * i]);
-  float l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int i = 0; i < a.splits; ++i) {
-    const float li = ml[2 * i + 1];
-    if (li == 0.0f) continue;                            // (this share saw nothing, and left no rows)
-    const float w = __builtin_amdgcn_exp2f(ml[2 * i] - m);
-    const float4 x = *(const float4*)(a.share_o + (place + i) * kHeadDim + 4 * sub);
-    l += w * li;
-    o[0] += w * x.x;
-    o[1] += w * x.y;
-    o[2] += w * x.z;
-    o[3] += w * x.w;
+  const float2* ml = (const float2*)a.share_ml + place;
+  const float4* shares = (const float4*)(a.share_o + place * kHeadDim) + sub;
+  float m = kNegBig, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int first = 0; first < a.splits; first += 32) {
+    const float2 own = first + sub < a.splits ? ml[first + sub] : make_float2(kNegBig, 0.0f);
+    const bool some = own.y != 0.0f;                     // (a share that saw nothing has left no rows)
+    float top = some ? own.x : kNegBig;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 32));
+    const float m_new = fmaxf(m, top), down = __builtin_amdgcn_exp2f(m - m_new);
+    m = m_new;
+    const float weight = some ? __builtin_amdgcn_exp2f(own.x - m) : 0.0f;
+    float sum = weight * own.y;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor(sum, off, 32);
+    l = l * down + sum;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] *= down;
+    const int count = min(32, a.splits - first);
+    for (int i0 = 0; i0 < count; i0 += 8) {
+      float4 x[8];
+      float w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        w[i] = __shfl(weight, i0 + i, 32);
+        x[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if (w[i] != 0.0f) x[i] = shares[(int64_t)(first + i0 + i) * (kHeadDim / 4)];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        o[0] += w[i] * x[i].x;
+        o[1] += w[i] * x[i].y;
+        o[2] += w[i] * x[i].z;
+        o[3] += w[i] * x[i].w;
+      }
+    }
   }
   const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
   half4 y;
