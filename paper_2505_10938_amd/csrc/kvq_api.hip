@@ -849,26 +849,47 @@ bool rows_ok(const void* p, int64_t stride, int64_t heads, int64_t head_dim) {
   return p && stride <= (1 << 23) && (((uintptr_t)p) & 15) == 0 && stride >= heads * head_dim && stride % 8 == 0;
 }
 
-// How a chunk's attention is dealt: row tiles of a unit, and workgroups that share a row tile's keys where the row tiles
-// alone would not fill the device (two workgroups fit a compute unit); each then has at least two tiles of 64 keys.
+// How a chunk's attention is dealt: wavefronts of 32 query rows per workgroup, row tiles of a unit, and workgroups that share a
+// row tile's keys.
+//  - Eight wavefronts share what it takes to bring a tile of keys (quantized ones are turned into fp16 rows), four leave less of
+//    a workgroup idle.  Four where the rows of a unit fit them and the units alone fill the device (us, four / eight: 64 sequences x
+//    32 tokens over 4000, 32 / 8 heads 203 / 276; 8 such sequences 51 / 48; 4 x 33 over 8000, 132 rows, 78 / 56; 64 x 60 over 300
+//    75 / 73), and where nothing is quantized and there are at most two rounds of the larger workgroups (prompts of 300 tokens
+//    15 / 18, 1000 30 / 37, 2 x 2000 with 32 kv heads 133 / 143; 4 x 4000 653 / 615, one of 8192 622 / 593).
+//  - A row tile's keys are shared out where there are at most half as many row tiles as compute units, to as many workgroups as
+//    there are compute units, two tiles of 64 keys each at least (4 tokens over 8000, 32 / 8 heads: 193 us with one workgroup each,
+//    36 / 27 / 20 / 28 with 16 / 11 / 4 / 2 tiles each; 33 tokens of 4 sequences 55 with 16 tiles each, 70 with 11).  With more row
+//    tiles than that it costs more than it gives: a workgroup that has a compute unit to itself is nearly as fast as two that
+//    share one (a prompt of 1000 tokens: 30 us, 36 with two workgroups each).
 struct ChunkShape {
-  int64_t row_tiles, splits;
+  int32_t waves;
+  int64_t row_tiles, most, splits;
+  int64_t unit_rows() const { return row_tiles * waves * kvq::kChunkWaveRows; }
 };
 ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quant, int64_t n_res, bool with_new) {
-  const int64_t g = cfg->q_heads / cfg->kv_heads;
+  const int64_t units = (int64_t)cfg->batch * cfg->kv_heads, unit_rows = max_tokens * (cfg->q_heads / cfg->kv_heads);
+  auto tiles_of = [&](int64_t waves) { return (unit_rows + waves * kvq::kChunkWaveRows - 1) / (waves * kvq::kChunkWaveRows); };
   ChunkShape s;
-  s.row_tiles = (max_tokens * g + kvq::kChunkRows - 1) / kvq::kChunkRows;
-  const int64_t groups = (int64_t)cfg->batch * cfg->kv_heads * s.row_tiles;
-  const int64_t rows = n_res + cfg->outlier_budget + cfg->aux_capacity;
-  const int64_t tiles = (n_quant + 63) / 64 + (rows + 63) / 64 + (with_new ? (max_tokens + 63) / 64 : 0);
-  s.splits = 2 * kvq::kComputeUnits / groups;
-  if (s.splits > tiles / 2) s.splits = tiles / 2;
+  const bool small = tiles_of(4) == 1 && units >= kvq::kComputeUnits;
+  const bool prompt = n_quant == 0 && units * tiles_of(8) <= 2 * kvq::kComputeUnits;
+  s.waves = small || prompt ? 4 : 8;
+  s.row_tiles = tiles_of(s.waves);
+  const int64_t fp_rows = n_res + cfg->outlier_budget + cfg->aux_capacity;
+  const int64_t held = (n_quant + 63) / 64 + (fp_rows + 63) / 64, own = with_new ? (max_tokens + 63) / 64 : 0;
+  const int64_t longest = held + own;
+  s.most = longest > 0 ? longest : 1;
+  if (2 * units * s.row_tiles <= kvq::kComputeUnits) {   // (of a causal chunk, row tiles have more keys the later they are)
+    const int64_t work = units * (s.row_tiles * held + s.row_tiles * (own + 1) / 2);
+    s.most = (work + kvq::kComputeUnits - 1) / kvq::kComputeUnits;
+    if (s.most < 2) s.most = 2;
+  }
+  s.splits = (longest + s.most - 1) / s.most;
   if (s.splits < 1) s.splits = 1;
   return s;
 }
 int64_t chunk_workspace_bytes(const kvq_config* cfg, const ChunkShape& s) {
   if (s.splits == 1) return 0;
-  return (int64_t)cfg->batch * cfg->kv_heads * s.row_tiles * kvq::kChunkRows * s.splits * (cfg->head_dim + 2) * 4;
+  return (int64_t)cfg->batch * cfg->kv_heads * s.unit_rows() * s.splits * (cfg->head_dim + 2) * 4;
 }
 
 }  // namespace
@@ -947,11 +968,13 @@ int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q
   a.n_res = n_res;
   a.g_shift = shift_of((int32_t)g);
   a.scale = 0.08838834764831845f * 1.4426950408889634f;
-  a.row_tiles = (int32_t)shape.row_tiles;
+  a.waves = shape.waves;
+  a.unit_rows = shape.unit_rows();
+  a.most = (int32_t)shape.most;
   a.splits = (int32_t)shape.splits;
   a.parts = parts;
   a.part_tiles = (int32_t)((shape.row_tiles + parts - 1) / parts);
-  const int64_t shares = items * kvq::kChunkRows;
+  const int64_t shares = units * shape.unit_rows() * shape.splits;
   a.share_o = (float*)workspace;
   a.share_ml = need > 0 ? a.share_o + shares * cfg->head_dim : nullptr;
   return from_hip(kvq::launch_prompt_attention(a, (hipStream_t)stream));

@@ -136,7 +136,7 @@ struct DecodeArgs {
 };
 
 // A chunk of new tokens against the caches of a batch (and against itself).
-constexpr int kChunkRows = 128;        // query rows, (token, query head) pairs of a kv head, of one workgroup
+constexpr int kChunkWaveRows = 32;      // query rows, (token, query head) pairs of a kv head, of one wavefront
 struct ChunkArgs {
   Dims d;
   const __half* q;
@@ -161,10 +161,12 @@ struct ChunkArgs {
   int32_t n_quant, res_start, n_res;
   int32_t g_shift;                      // query heads per kv head = 1 << g_shift
   float scale;                          // 1 / sqrt(head_dim) * log2(e): scores are kept in powers of two
-  int32_t row_tiles;                    // workgroups per unit along the query rows, of max_tokens tokens
-  int32_t splits;                       // workgroups that share a row tile's keys
+  int32_t waves;                        // of a workgroup: 4 or 8
+  int64_t unit_rows;                    // rows of a unit in the shares: row tiles times rows of a workgroup
+  int32_t most;                         // tiles of 64 keys of one workgroup, at most: a row tile with more is shared
+  int32_t splits;                       // by so many workgroups at most
   int32_t parts;                        // 1, 2, 4 or 8: units * parts is a multiple of 8
-  int32_t part_tiles;                   // row tiles of a part of a unit: row_tiles / parts, rounded up
+  int32_t part_tiles;                   // row tiles of a part of a unit, rounded up
   float* share_ml;                      // splits > 1: [unit][row][split][2] maximum (log2) and sum of a row's share
   float* share_o;                       //             [unit][row][split][head_dim]
 };

@@ -19,11 +19,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kTile = 64;            // keys per tile
-constexpr int kWaves = 4;
-constexpr int kThreads = 64 * kWaves;
-constexpr int kWaveRows = 32;        // query rows of a wavefront: (token, query head) pairs, token-major
-constexpr int kRows = kChunkRows;
-static_assert(kRows == kWaves * kWaveRows, "a workgroup's rows are its wavefronts'");
+constexpr int kMergeThreads = 256;
+constexpr int kWaveRows = kChunkWaveRows;   // query rows of a wavefront: (token, query head) pairs, token-major
 constexpr int kPitchK = 272;         // LDS rows of 128 fp16: 16 bytes more, so that 16 rows' 16-byte pieces lie in different banks
 constexpr int kPitchV = 320;         // four rows' 64-byte pieces in different banks
 constexpr int kPitchT = 144;         // LDS rows of 64 keys of one channel
@@ -51,17 +48,16 @@ __device__ __forceinline__ uint32_t dequant_pair(uint32_t w, uint32_t step, uint
   return as_u32(__builtin_elementwise_fma(code, as_h2(step), as_h2(zero)));
 }
 template <int BITS>
-__device__ __forceinline__ u32x4 dequant_field(const uint32_t (&w)[2 * BITS], int f, const uint32_t (&step)[4],
-                                               const uint32_t (&zero)[4]) {
+__device__ __forceinline__ u32x4 dequant_field(uint32_t word, int odd, const uint32_t (&step)[4], const uint32_t (&zero)[4]) {
   u32x4 r;
-  if (BITS == 2) {
-    const uint32_t word = (f & 1) ? rotr32(w[f >> 1], 8) : w[f >> 1];
-    r[0] = dequant_pair<2, 0>(word, step[0], zero[0]);
-    r[1] = dequant_pair<2, 1>(word, step[1], zero[1]);
-    r[2] = dequant_pair<2, 2>(word, step[2], zero[2]);
-    r[3] = dequant_pair<2, 3>(word, step[3], zero[3]);
+  if (BITS == 2) {                                       // (`odd`: the second field of the word)
+    const uint32_t w = odd ? rotr32(word, 8) : word;
+    r[0] = dequant_pair<2, 0>(w, step[0], zero[0]);
+    r[1] = dequant_pair<2, 1>(w, step[1], zero[1]);
+    r[2] = dequant_pair<2, 2>(w, step[2], zero[2]);
+    r[3] = dequant_pair<2, 3>(w, step[3], zero[3]);
   } else {
-    const uint32_t word = w[f], high = rotr32(word, 8);
+    const uint32_t high = rotr32(word, 8);
     r[0] = dequant_pair<4, 0>(word, step[0], zero[0]);
     r[1] = dequant_pair<4, 1>(word, step[1], zero[1]);
     r[2] = dequant_pair<4, 2>(high, step[2], zero[2]);
@@ -80,19 +76,72 @@ __device__ __forceinline__ float other_half(float v) {
   return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
-// What a wavefront loads for the next tile of quantized tokens: one block's Keys (wavefronts 0, 1) or Values (2, 3).
-template <int BITS, int NV>
+// What a wavefront loads for the next tile of quantized tokens: a half or (NW = 8) a quarter of a block's codes, steps and zeros.
+// It has F = 8 / NW times two fields of the Keys (cb = F part .., both halves of the tokens) and as many of the Values (ct =
+// 2 F part ..).
+template <int BITS, int NV, int F>
 struct QuantRegs {
-  u32x4 codes[BITS / 2];
-  u32x4 step[4], zero[4];              // Keys: of the channels of the lane's four fields; Values: [pair][value group]
+  static constexpr int kVGroups = NV == 4 && F == 2 ? 2 : 1;
+  uint32_t k[2][BITS == 2 ? 1 : F];    // [half of the tokens][2-bit: the word, 4-bit: field]
+  uint32_t v[BITS == 2 ? F : 2 * F];   // 2-bit: two fields a word
+  u32x4 k_step[F], k_zero[F];          // of a field's eight channels
+  uint32_t v_step[4][kVGroups], v_zero[4][kVGroups];     // of token pair 4 r + v
 };
+template <int N>
+__device__ __forceinline__ void load_words(uint32_t (&w)[N], const unsigned char* p) {
+  if constexpr (N == 1) {
+    w[0] = *(const uint32_t*)p;
+  } else if constexpr (N == 2) {
+    const u32x2 x = *(const u32x2*)p;
+    w[0] = x[0], w[1] = x[1];
+  } else {
+    const u32x4 x = *(const u32x4*)p;
+    w[0] = x[0], w[1] = x[1], w[2] = x[2], w[3] = x[3];
+  }
+}
+
+// What a sequence holds, and the keys of a row tile, 64 a tile, in this order: quantized tokens; new tokens that every row of
+// the tile sees; full-precision rows of the cache; the other new tokens.
+struct CacheRows {
+  int nq, rs, nr, n_pool, n_aux;
+};
+__device__ __forceinline__ CacheRows cache_rows(const ChunkArgs& a, int b, int64_t u) {
+  const Dims& d = a.d;
+  CacheRows c = {a.n_quant, a.res_start, a.n_res, 0, 0};
+  if (a.seq) {
+    const int4 own = *(const int4*)(a.seq + 4 * b);
+    c.nq = min(max(own.x, 0), a.n_quant) & ~(kBlockTokens - 1);
+    c.rs = own.y >= 0 && own.y < d.res_rows ? own.y : 0;
+    c.nr = min(max(own.z, 0), a.n_res);
+  }
+  if (d.N > 0) {
+    c.n_pool = min(max(a.pool_count[u], 0), d.N);
+    c.n_aux = min(max(a.aux_count[u], 0), d.A);
+  }
+  return c;
+}
+struct TileKeys {
+  int n_new, tq, ti, tr, tiles;
+  int splits;                // workgroups that share them: as few as have a.most tiles each
+};
+__device__ __forceinline__ TileKeys tile_keys(const ChunkArgs& a, const CacheRows& c, int n, int first_row, int live_rows) {
+  TileKeys k;
+  k.n_new = a.k_new ? min(n, ((first_row + live_rows - 1) >> a.g_shift) + 1) : 0;
+  k.tq = (c.nq + kTile - 1) / kTile;
+  k.ti = a.k_new ? min(n, (first_row >> a.g_shift) + 1) / kTile : 0;
+  k.tr = (c.n_pool + c.n_aux + c.nr + kTile - 1) / kTile;
+  k.tiles = k.tq + k.tr + (k.n_new + kTile - 1) / kTile;
+  k.splits = max((k.tiles + a.most - 1) / a.most, 1);
+  return k;
+}
 
 // One wavefront has 32 query rows, whose products with 64 keys stand transposed in its registers (keys down, one query row
 // per lane and half): the softmax of a row is then work inside a lane, and the weights are, as they stand, an operand of the
 // second product if its keys are taken in the order in which the first one leaves them (16 s + 8 (j / 4) + 4 h + j % 4 for half
 // h of the lanes, element j).  Four wavefronts share the keys' and values' tiles in LDS, two buffers.
-template <int BITS, int NV>
-__global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs a) {
+template <int BITS, int NV, int NW>
+__global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs a) {
+  constexpr int kRows = NW * kWaveRows;
   extern __shared__ __align__(16) unsigned char smem[];
   const Dims& d = a.d;
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, col = lane & 31;
@@ -110,33 +159,22 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
   const int tile_back = tile_in_part * a.parts + (part_unit - ul * a.parts);
   const int b = ul / d.kv_heads, h = ul - b * d.kv_heads;
   const ChunkRows mine = chunk_rows(a.starts, a.total, a.max_tokens, b);
-  const int64_t s0 = mine.first;
+  const int64_t s0 = mine.first, u = d.unit0 + ul;
   const int n = mine.n;
   const int row_tiles = (int)(((int64_t)n * d.g + kRows - 1) / kRows);
   if (tile_back >= row_tiles) return;
   const int row_tile = row_tiles - 1 - tile_back;        // the longest ones first
-  int nq = a.n_quant, rs = a.res_start, nr = a.n_res;
-  if (a.seq) {
-    const int4 own = *(const int4*)(a.seq + 4 * b);
-    nq = min(max(own.x, 0), a.n_quant) & ~(kBlockTokens - 1);
-    rs = (own.y >= 0 && own.y < d.res_rows) ? own.y : 0;
-    nr = min(max(own.z, 0), a.n_res);
-  }
-  const int64_t u = d.unit0 + ul;
-  const int n_pool = d.N > 0 ? min(max(a.pool_count[u], 0), d.N) : 0;
-  const int n_aux = d.N > 0 ? min(max(a.aux_count[u], 0), d.A) : 0;
-  const int n_rows = n_pool + n_aux + nr;                // full-precision rows of the cache
   const int first_row = row_tile * kRows;                // of the unit's n * g rows
   const int live_rows = (int)min((int64_t)kRows, (int64_t)n * d.g - first_row);
-  const int first_token = first_row >> a.g_shift;
-  const int n_new = a.k_new ? min(n, ((first_row + live_rows - 1) >> a.g_shift) + 1) : 0;
-  // Tiles, in this order: quantized tokens; new tokens that every row of the workgroup sees; full-precision rows of the
-  // cache; the other new tokens.
-  const int tq = (nq + kTile - 1) / kTile, tr = (n_rows + kTile - 1) / kTile;
-  const int ti = a.k_new ? min(n, first_token + 1) / kTile : 0, tn = (n_new + kTile - 1) / kTile - ti;
-  const int tiles = tq + ti + tr + tn;
-  const int per = (tiles + a.splits - 1) / a.splits;
-  const int t_begin = min(split * per, tiles), t_end = min(t_begin + per, tiles);
+  const CacheRows held = cache_rows(a, b, u);
+  const int nq = held.nq, rs = held.rs, n_pool = held.n_pool, n_aux = held.n_aux;
+  const int n_rows = n_pool + n_aux + held.nr;           // full-precision rows of the cache
+  const TileKeys keys = tile_keys(a, held, n, first_row, live_rows);
+  const int first_token = first_row >> a.g_shift, n_new = keys.n_new, tq = keys.tq, ti = keys.ti, tr = keys.tr;
+  const int my_splits = keys.splits;
+  if (split >= my_splits) return;
+  const int per = (keys.tiles + my_splits - 1) / my_splits;
+  const int t_begin = min(split * per, keys.tiles), t_end = min(t_begin + per, keys.tiles);
 
   // ---- the wavefront's query rows, as a matrix operand: lane (row col, channels 16 s + 8 half ..)
   const int wave_row = first_row + wave * kWaveRows;
@@ -165,8 +203,11 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
 
   // First product, softmax, second product of one tile.  V stands as rows of channels (two transposing reads bring four keys
   // each of a channel to a lane) or, dequantized, already by channel in the order of the second product.  `hide(x)` sets the
-  // scores of keys that a row does not see to -infinity, `keep(p)` may look at the weights.
-  auto compute = [&](auto quantized, const unsigned char* buf, auto hide, auto keep) {
+  // scores of keys that a row does not see to -infinity, `keep(p)` may look at the weights.  `ask()` may ask for the next tile
+  // between the first product's matrix instructions, `put(s)` store a quarter of it into the other buffer behind each quarter
+  // of the second product.  (That is for quantized tiles, which take instructions to store: 16 sequences of different lengths,
+  // 4-bit codes, 430 us with all of it behind the tile and a wavefront either Keys or Values, 345 so.  With fp16 rows it is even.)
+  auto compute = [&](auto quantized, const unsigned char* buf, auto ask, auto hide, auto keep, auto put) {
     constexpr bool QUANT = decltype(quantized)::value;
     const unsigned char* sk = buf + col * kPitchK + 16 * half;
     const unsigned char* sv = buf + kBytesK;
@@ -189,6 +230,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
     for (int s = 0; s < 8; ++s)
 #pragma unroll
       for (int t = 0; t < 2; ++t) k[2 * s + t] = *(const half8*)(sk + 32 * t * kPitchK + 32 * s);
+    ask();
 #pragma unroll
     for (int s = 0; s < 8; ++s)
 #pragma unroll
@@ -201,9 +243,12 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
-    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, QUANT ? 4 : 8, 0);
-    __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (i == 4) __builtin_amdgcn_sched_group_barrier(0x100, QUANT ? 4 : 8, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      if (QUANT) __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);
+    }
     __builtin_amdgcn_s_setprio(0);
     hide(x);
     float top = largest(x[0][0], x[1][0]);
@@ -239,22 +284,23 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
 #pragma unroll
       for (int c = 0; c < 4; ++c)
         o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s == 0 ? v0[c] : value(s, c), weights, o[c], 0, 0, 0);
+      put(s);
     }
   };
-  const auto nothing = [](auto&) {};
+  const auto nothing = [](auto&&...) {};
 
-  // ---- quantized tokens, 64 (two blocks) a tile: each wavefront turns one block's Keys or Values into fp16 rows
+  // ---- quantized tokens, 64 (two blocks) a tile: each wavefront turns its share of a block's Keys and Values into fp16 rows
   {
-    const int which = wave >> 1;                         // 0: Keys, 1: Values
     const int last = (nq >> 5) - 1;
     const int qe = min(t_end, tq);
-    const int r = lane >> 4, m16 = lane & 15;
-    QuantRegs<BITS, NV> R;
+    const int r = lane >> 4, m16 = lane & 15, part = wave >> 1;
+    constexpr int F = 8 / NW;
+    QuantRegs<BITS, NV, F> R;
     uint32_t mask0 = 0, mask1 = 0;
     // The page numbers of 64 groups at a time, a lane each: a look into the table for every tile would have the tile's loads
     // wait for it.
     int pages = 0, first_group = -64;
-    auto place = [&](int blk) -> GroupPlace {            // (called with ascending blocks, but for those of one tile)
+    auto place = [&](int blk) -> GroupPlace {            // (called with ascending blocks)
       const int group = blk >> d.bpg_shift;
       if (!d.page_table) return {u, group};
       if (group - first_group >= 64) {                   // uniform
@@ -264,113 +310,137 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
       const int page = __builtin_amdgcn_readlane(pages, group - first_group);
       return {d.plane0 + h, min(max(page, 0), d.n_pages - 1)};
     };
-    auto load = [&](int tile) {
+    // Where the wavefront's share of a tile is.
+    const unsigned char* at_k = nullptr;
+    const unsigned char* at_v = nullptr;
+    const unsigned char* at_km = nullptr;
+    const unsigned char* at_vm = nullptr;
+    const uint32_t* at_mask[2] = {nullptr, nullptr};
+    auto find = [&](int tile) {
       const int b0 = 2 * tile, b1 = min(2 * tile + 1, last);     // (behind the last block: that one again, all of it hidden)
+      const int in_group = (1 << d.bpg_shift) - 1;
       const GroupPlace g0 = place(b0), g1 = place(b1);
-      const int blk = (wave & 1) ? b1 : b0;
-      const GroupPlace at = (wave & 1) ? g1 : g0;
-      const int64_t pblk = at.row * d.blocks_per_unit + ((int64_t)at.slot << d.bpg_shift) + (blk & ((1 << d.bpg_shift) - 1));
-      const u32x4* codes = (const u32x4*)((which ? a.v_codes : a.k_codes) + pblk * d.block_bytes);
+      const int64_t p0 = g0.row * d.blocks_per_unit + ((int64_t)g0.slot << d.bpg_shift) + (b0 & in_group);
+      const int64_t p1 = g1.row * d.blocks_per_unit + ((int64_t)g1.slot << d.bpg_shift) + (b1 & in_group);
+      const int64_t blk = (wave & 1) ? p1 : p0, group = (wave & 1) ? g1.row * d.groups_per_unit + g1.slot : g0.row * d.groups_per_unit + g0.slot;
+      const int cb = F * part, ct = 2 * F * part;        // first fields
+      at_k = a.k_codes + blk * d.block_bytes + (BITS == 2 ? 4 * (cb >> 1) : 4 * cb);
+      at_v = a.v_codes + blk * d.block_bytes + (BITS == 2 ? 4 * (ct >> 1) : 1024 * (ct >> 2) + 4 * (ct & 3));
+      at_km = a.k_meta + group * 512 + 64 * cb;
+      at_vm = a.v_meta + blk * (128 * NV) + 4 * (ct * NV / 8);
+      at_mask[0] = a.mask + p0;
+      at_mask[1] = a.mask + p1;
+    };
+    auto load = [&]() {
 #pragma unroll
-      for (int i = 0; i < BITS / 2; ++i) R.codes[i] = codes[64 * i + lane];
-      if (which == 0) {
-        const unsigned char* meta = a.k_meta + (at.row * d.groups_per_unit + at.slot) * 512 + 16 * r;
+      for (int th = 0; th < 2; ++th) load_words(R.k[th], at_k + 16 * lane + (BITS == 2 ? 8 : 1024) * th);
+      load_words(R.v, at_v + 16 * lane);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          R.step[i] = *(const u32x4*)(meta + 64 * i);
-          R.zero[i] = *(const u32x4*)(meta + 64 * i + 256);
+      for (int e = 0; e < F; ++e) {
+        R.k_step[e] = *(const u32x4*)(at_km + 64 * e + 16 * r);
+        R.k_zero[e] = *(const u32x4*)(at_km + 64 * e + 16 * r + 256);
+      }
+      if constexpr (NV == 1) {
+        const u32x4 st = *(const u32x4*)(at_vm + 16 * r), ze = *(const u32x4*)(at_vm + 16 * r + 64);
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+          R.v_step[v][0] = st[v];
+          R.v_zero[v][0] = ze[v];
         }
       } else {
-        const unsigned char* meta = a.v_meta + pblk * (128 * NV) + 16 * NV * r;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-          R.step[i] = *(const u32x4*)(meta + 16 * i);
-          R.zero[i] = *(const u32x4*)(meta + 16 * i + 64 * NV);
+        for (int v = 0; v < 4; ++v) {                    // pair 4 r + v, the value groups of this part of the channels
+          load_words(R.v_step[v], at_vm + 4 * NV * (4 * r + v));
+          load_words(R.v_zero[v], at_vm + 4 * NV * (4 * r + v) + 64 * NV);
         }
       }
-      // (every wavefront wants both blocks' mask words)
-      const int in_group = (1 << d.bpg_shift) - 1;
-      mask0 = a.mask[g0.row * d.blocks_per_unit + ((int64_t)g0.slot << d.bpg_shift) + (b0 & in_group)];
-      mask1 = a.mask[g1.row * d.blocks_per_unit + ((int64_t)g1.slot << d.bpg_shift) + (b1 & in_group)];
+      mask0 = *at_mask[0];                               // (every wavefront wants both blocks' mask words)
+      mask1 = *at_mask[1];
     };
-    auto store = [&](unsigned char* buf) {
-      const int at = 32 * (wave & 1);                    // the block's tokens of the tile
-      uint32_t w[2 * BITS];
+    // Piece s of the share's 2 F: a field of Keys (8 channels from 32 cb + 8 r on of token 16 th + m16) and one of Values (tokens
+    // 8 r .. of channel 16 ct + m16).
+    auto put_piece = [&](unsigned char* buf, int s) {
+      if (s >= 2 * F) return;
+      const int token0 = 32 * (wave & 1), e = F == 2 ? s & 1 : 0, th = F == 2 ? s >> 1 : s;
+      {
+        uint32_t st[4], ze[4];
 #pragma unroll
-      for (int i = 0; i < 2 * BITS; ++i) w[i] = R.codes[i >> 2][i & 3];
-      if (which == 0) {                                  // field 4 th + cb: 8 channels from 32 cb + 8 r on of token 16 th + m16
-        unsigned char* sk = buf + (at + m16) * kPitchK + 16 * r;
-#pragma unroll
-        for (int f = 0; f < 8; ++f) {
-          uint32_t st[4], ze[4];
-#pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            st[v] = R.step[f & 3][v];
-            ze[v] = R.zero[f & 3][v];
-          }
-          *(u32x4*)(sk + 16 * (f >> 2) * kPitchK + 64 * (f & 3)) = dequant_field<BITS>(w, f, st, ze);
+        for (int v = 0; v < 4; ++v) {
+          st[v] = R.k_step[e][v];
+          ze[v] = R.k_zero[e][v];
         }
-      } else {                                           // field ct: tokens 8 r .. of channel 16 ct + m16
-        unsigned char* sv = buf + kBytesK + m16 * kPitchT + 2 * (at + 16 * (r >> 1) + 4 * (r & 1));
+        const int odd = BITS == 2 ? (F == 2 ? e : part & 1) : 0;
+        *(u32x4*)(buf + (token0 + 16 * th + m16) * kPitchK + 64 * F * part + 64 * e + 16 * r) =
+            dequant_field<BITS>(R.k[th][BITS == 2 ? 0 : e], odd, st, ze);
+      }
+      {
+        constexpr int kOf = F == 2 ? 1 : 0;
+        uint32_t st[4], ze[4];
 #pragma unroll
-        for (int f = 0; f < 8; ++f) {
-          constexpr int kFieldsPerGroup = 8 / NV;
-          uint32_t st[4], ze[4];
+        for (int v = 0; v < 4; ++v) {
+          st[v] = R.v_step[v][NV == 4 && kOf ? s >> 1 : 0];
+          ze[v] = R.v_zero[v][NV == 4 && kOf ? s >> 1 : 0];
+        }
+        const u32x4 x = dequant_field<BITS>(R.v[BITS == 2 ? s >> 1 : s], BITS == 2 ? s & 1 : 0, st, ze);
+        unsigned char* sv = buf + kBytesK + (32 * F * part + 16 * s + m16) * kPitchT + 2 * (token0 + 16 * (r >> 1) + 4 * (r & 1));
+        *(u32x2*)sv = u32x2{x[0], x[1]};
+        *(u32x2*)(sv + 16) = u32x2{x[2], x[3]};
+      }
+    };
+    auto put_all = [&](unsigned char* buf) {
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            const int i = v * NV + f / kFieldsPerGroup;
-            st[v] = R.step[i >> 2][i & 3];
-            ze[v] = R.zero[i >> 2][i & 3];
-          }
-          const u32x4 x = dequant_field<BITS>(w, f, st, ze);
-          *(u32x2*)(sv + 16 * f * kPitchT) = u32x2{x[0], x[1]};
-          *(u32x2*)(sv + 16 * f * kPitchT + 16) = u32x2{x[2], x[3]};
+      for (int s = 0; s < 2 * F; ++s) put_piece(buf, s);
+    };
+    uint32_t hidden[2];
+    auto hide = [&](float16v (&x)[2]) {
+      if (hidden[0] | hidden[1]) {                       // uniform
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t word = hidden[i] >> (4 * half);
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (word & (1u << (8 * (r >> 2) + (r & 3)))) x[i][r] = -__builtin_inff();
         }
       }
+    };
+    // (the words are looked at when the tile is, not when they are asked for: everything would wait for them)
+    auto look = [&](int tile) {
+      hidden[0] = __builtin_amdgcn_readfirstlane(mask0);
+      hidden[1] = 2 * tile + 1 > last ? ~0u : (uint32_t)__builtin_amdgcn_readfirstlane(mask1);
     };
     if (t_begin < qe) {
-      // (the words are looked at when the tile is, not when they are asked for: everything would wait for them)
-      auto second = [&](int tile) { return 2 * tile + 1 > last ? ~0u : mask1; };
-      load(t_begin);
-      uint32_t h0 = mask0, h1 = second(t_begin);
-      store(buffer);
+      find(t_begin);
+      load();
+      put_all(buffer);
+      look(t_begin);
       __syncthreads();
-      for (int t = t_begin; t < qe; ++t) {
-        const bool more = t + 1 < qe;
-        if (more) load(t + 1);
+      for (int t = t_begin; t + 1 < qe; ++t) {
+        find(t + 1);
+        unsigned char* next = other(buffer);
         if (wave_live) {
-          const uint32_t hidden[2] = {(uint32_t)__builtin_amdgcn_readfirstlane(h0), (uint32_t)__builtin_amdgcn_readfirstlane(h1)};
-          compute(std::true_type{}, buffer, [&](float16v (&x)[2]) {
-            if (hidden[0] | hidden[1]) {                 // uniform
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const uint32_t word = hidden[i] >> (4 * half);
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                  if (word & (1u << (8 * (r >> 2) + (r & 3)))) x[i][r] = -__builtin_inff();
-              }
-            }
-          }, nothing);
+          compute(std::true_type{}, buffer, load, hide, nothing, [&](int s) { put_piece(next, s); });
+        } else {
+          load();
+          put_all(next);
         }
-        buffer = other(buffer);
-        if (more) {
-          store(buffer);
-          h0 = mask0;
-          h1 = second(t + 1);
-        }
+        look(t + 1);
+        buffer = next;
         __syncthreads();
       }
+      if (wave_live) compute(std::true_type{}, buffer, nothing, hide, nothing, nothing);
+      buffer = other(buffer);
     }
   }
 
   // ---- full-precision rows, 64 a tile
   const int piece = tid & 15, line = tid >> 4;
-  u32x4 rk[4], rv[4];
+  constexpr int kPasses = 16 / NW, kLines = 4 * NW;      // rows of a tile: kLines at a time
+  u32x4 rk[kPasses], rv[kPasses];
   auto store = [&](unsigned char* buf) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      *(u32x4*)(buf + (16 * i + line) * kPitchK + 16 * piece) = rk[i];
-      *(u32x4*)(buf + kBytesK + (16 * i + line) * kPitchV + 16 * piece) = rv[i];
+    for (int i = 0; i < kPasses; ++i) {
+      *(u32x4*)(buf + (kLines * i + line) * kPitchK + 16 * piece) = rk[i];
+      *(u32x4*)(buf + kBytesK + (kLines * i + line) * kPitchV + 16 * piece) = rv[i];
     }
   };
 
@@ -385,22 +455,23 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
         const unsigned char* pk = (const unsigned char*)a.k_new + at;
         const unsigned char* pv = (const unsigned char*)a.v_new + at;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          rk[i] = *(const u32x4*)(pk + (offset + 16 * i * row_bytes));
-          rv[i] = *(const u32x4*)(pv + (offset + 16 * i * row_bytes));
+        for (int i = 0; i < kPasses; ++i) {
+          rk[i] = *(const u32x4*)(pk + (offset + kLines * i * row_bytes));
+          rv[i] = *(const u32x4*)(pv + (offset + kLines * i * row_bytes));
         }
       };
       load(nb);
       store(buffer);
       __syncthreads();
-      for (int t = nb; t < ne; ++t) {
-        const bool more = t + 1 < ne;
-        if (more) load(t + 1);
-        if (wave_live) compute(std::false_type{}, buffer, nothing, nothing);
+      for (int t = nb; t + 1 < ne; ++t) {
+        load(t + 1);
+        if (wave_live) compute(std::false_type{}, buffer, nothing, nothing, nothing, nothing);
         buffer = other(buffer);
-        if (more) store(buffer);
+        store(buffer);
         __syncthreads();
       }
+      if (wave_live) compute(std::false_type{}, buffer, nothing, nothing, nothing, nothing);
+      buffer = other(buffer);
     }
   }
 
@@ -419,8 +490,8 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
       const bool own = tile >= rows_end;                 // uniform
       const int first = own ? (tile - rows_end + ti) * kTile : (tile - tq - ti) * kTile;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int e = first + 16 * i + line;
+      for (int i = 0; i < kPasses; ++i) {
+        const int e = first + kLines * i + line;
         rk[i] = rv[i] = u32x4{0, 0, 0, 0};
         const __half* fk;
         const __half* fv;
@@ -445,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
     auto sort_out = [&]() {
       uint32_t odd = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < kPasses; ++i)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const uint32_t w = rv[i][k], lo = (w & 0x7C00u) == 0x7C00u ? 0xFFFFu : 0u, hi = (w & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u;
@@ -454,21 +525,33 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
         }
       return odd;
     };
-    // The Values left out of a tile, for the rows that see them.  Weights have gone through LDS (the buffer that is not in use).
-    auto late = [&](int tile, int limit, const float* mine) {
+    // The Values left out of a tile, for the rows that see them.  Weights of half the keys at a time go through LDS (the buffer
+    // that is not in use).
+    auto late = [&](int tile, int limit, float* mine, const float16v (&x)[2]) {
+      static_assert(NW * kWaveRows * 32 * 4 <= kBytesBuffer, "the weights of all wavefronts have room in a buffer");
       const int base = (tile - rows_end + ti) * kTile;
-      for (int k = 0; k < kTile && base + k < n_new; ++k) {
-        const float w = mine[k * kWaveRows + col];
-        const __half* vr = a.v_new + (s0 + base + k) * a.kv_stride + h * kHeadDim + 4 * half;
 #pragma unroll
-        for (int c = 0; c < 4; ++c)
+      for (int t = 0; t < 2; ++t) {
 #pragma unroll
-          for (int r4 = 0; r4 < 4; ++r4) {
-            const half4 v = *(const half4*)(vr + 32 * c + 8 * r4);
+        for (int r = 0; r < 16; ++r) mine[(8 * (r >> 2) + 4 * half + (r & 3)) * kWaveRows + col] = x[t][r];
+        __builtin_amdgcn_s_waitcnt(0xc07f);              // lgkmcnt(0): the wavefront's own stores
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+        for (int k = 32 * t; k < 32 * t + 32 && base + k < n_new; ++k) {
+          const float w = mine[(k & 31) * kWaveRows + col];
+          const __half* vr = a.v_new + (s0 + base + k) * a.kv_stride + h * kHeadDim + 4 * half;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (k < limit && w != 0.0f && !(fabsf((float)v[i]) <= 65504.0f)) o[c][4 * r4 + i] += w * (float)v[i];
-          }
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+              const half4 v = *(const half4*)(vr + 32 * c + 8 * r4);
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (k < limit && w != 0.0f && !(fabsf((float)v[i]) <= 65504.0f)) o[c][4 * r4 + i] += w * (float)v[i];
+            }
+        }
+        __builtin_amdgcn_s_waitcnt(0xc07f);
+        __builtin_amdgcn_wave_barrier();
       }
     };
     if (fb < t_end) {
@@ -485,26 +568,15 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
         const int limit = (own ? min(n_new, token + 1) : n_rows) - base;
         const int most = (own ? min(n_new, ((wave_row + kWaveRows - 1) >> a.g_shift) + 1) : n_rows) - base;
         if (wave_live && most > 0) {
-          float* mine = (float*)(other(buffer) + wave * (kWaveRows * kTile * 4));
-          compute(std::false_type{}, buffer, [&](float16v (&x)[2]) {
+          compute(std::false_type{}, buffer, nothing, [&](float16v (&x)[2]) {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
               for (int r = 0; r < 16; ++r)
                 if (32 * i + 8 * (r >> 2) + (r & 3) + 4 * half >= limit) x[i][r] = -__builtin_inff();
           }, [&](float16v (&x)[2]) {
-            if (odd) {                                   // uniform
-#pragma unroll
-              for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) mine[(32 * i + 8 * (r >> 2) + 4 * half + (r & 3)) * kWaveRows + col] = x[i][r];
-            }
-          });
-          if (odd) {
-            __builtin_amdgcn_s_waitcnt(0xc07f);          // lgkmcnt(0): the wavefront's own stores
-            __builtin_amdgcn_wave_barrier();
-            late(t, limit, mine);
-          }
+            if (odd) late(t, limit, (float*)(other(buffer) + wave * (kWaveRows * 32 * 4)), x);     // (uniform)
+          }, nothing);
         }
         buffer = other(buffer);
         if (more) {
@@ -520,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
   // ---- the rows' results: normalized, or this split's share
   if (!row_live) return;
   l += other_half(l);
-  if (a.splits == 1) {
+  if (my_splits == 1) {
     const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
     __half* to = a.out + ((s0 + token) * d.q_heads + head) * kHeadDim + 4 * half;
 #pragma unroll
@@ -534,7 +606,7 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
       }
     return;
   }
-  const int64_t place = (((int64_t)ul * a.row_tiles + row_tile) * kRows + (row - first_row)) * a.splits + split;
+  const int64_t place = ((int64_t)ul * a.unit_rows + row) * a.splits + split;
   if (half == 0) *(float2*)(a.share_ml + 2 * place) = make_float2(m, l);
   if (l == 0.0f) return;
   float* to = a.share_o + place * kHeadDim + 4 * half;
@@ -547,21 +619,24 @@ __global__ void __launch_bounds__(kThreads, 2) prompt_attention_kernel(ChunkArgs
 
 // The shares of a row's splits put together: sum of 2^(m_i - max m) (l_i, o_i).  32 lanes a row: a lane has the maximum and the
 // sum of one of 32 splits, and four channels; the splits' rows are asked for eight at a time.
-__global__ void __launch_bounds__(kThreads) prompt_merge_kernel(ChunkArgs a) {
+__global__ void __launch_bounds__(kMergeThreads) prompt_merge_kernel(ChunkArgs a) {
   const Dims& d = a.d;
   const int sub = threadIdx.x & 31;
-  const int row = blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
+  const int row = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5);
   const int h = blockIdx.y, b = blockIdx.z, ul = b * d.kv_heads + h;
   const ChunkRows mine = chunk_rows(a.starts, a.total, a.max_tokens, b);
   const int64_t s0 = mine.first;
   const int n = mine.n;
   if (row >= (int64_t)n * d.g) return;
-  const int64_t place = ((int64_t)ul * a.row_tiles * kRows + row) * a.splits;
+  const int rows = a.waves * kWaveRows, first_row = row / rows * rows;
+  const int splits = tile_keys(a, cache_rows(a, b, d.unit0 + ul), n, first_row, (int)min((int64_t)rows, (int64_t)n * d.g - first_row)).splits;
+  if (splits == 1) return;                               // (written by the workgroup that had them all)
+  const int64_t place = ((int64_t)ul * a.unit_rows + row) * a.splits;
   const float2* ml = (const float2*)a.share_ml + place;
   const float4* shares = (const float4*)(a.share_o + place * kHeadDim) + sub;
   float m = kNegBig, l = 0.0f, o[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  for (int first = 0; first < a.splits; first += 32) {
-    const float2 own = first + sub < a.splits ? ml[first + sub] : make_float2(kNegBig, 0.0f);
+  for (int first = 0; first < splits; first += 32) {
+    const float2 own = first + sub < splits ? ml[first + sub] : make_float2(kNegBig, 0.0f);
     const bool some = own.y != 0.0f;                     // (a share that saw nothing has left no rows)
     float top = some ? own.x : kNegBig;
 #pragma unroll
@@ -575,7 +650,7 @@ __global__ void __launch_bounds__(kThreads) prompt_merge_kernel(ChunkArgs a) {
     l = l * down + sum;
 #pragma unroll
     for (int i = 0; i < 4; ++i) o[i] *= down;
-    const int count = min(32, a.splits - first);
+    const int count = min(32, splits - first);
     for (int i0 = 0; i0 < count; i0 += 8) {
       float4 x[8];
       float w[8];
@@ -610,21 +685,21 @@ hipError_t launch_prompt_attention(const ChunkArgs& a, hipStream_t s) {
   auto go = [&](auto kern) {
     hipError_t e = hipFuncSetAttribute((const void*)kern, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * kBytesBuffer);
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL(kern, dim3(grid), dim3(kThreads), 2 * kBytesBuffer, s, a);
+    hipLaunchKernelGGL(kern, dim3(grid), dim3(64 * a.waves), 2 * kBytesBuffer, s, a);
     return hipGetLastError();
   };
   auto of_bits = [&](auto bits) {
     constexpr int BITS = decltype(bits)::value;
     switch (a.d.vgroups) {
-      case 4: return go(prompt_attention_kernel<BITS, 4>);
-      case 2: return go(prompt_attention_kernel<BITS, 2>);
-      default: return go(prompt_attention_kernel<BITS, 1>);
+      case 4: return a.waves == 8 ? go(prompt_attention_kernel<BITS, 4, 8>) : go(prompt_attention_kernel<BITS, 4, 4>);
+      case 2: return a.waves == 8 ? go(prompt_attention_kernel<BITS, 2, 8>) : go(prompt_attention_kernel<BITS, 2, 4>);
+      default: return a.waves == 8 ? go(prompt_attention_kernel<BITS, 1, 8>) : go(prompt_attention_kernel<BITS, 1, 4>);
     }
   };
   hipError_t e = a.d.bits == 2 ? of_bits(std::integral_constant<int, 2>{}) : of_bits(std::integral_constant<int, 4>{});
   if (e != hipSuccess || a.splits == 1) return e;
   const int64_t rows = (int64_t)a.max_tokens * a.d.g;
-  hipLaunchKernelGGL(prompt_merge_kernel, dim3((uint32_t)((rows + 7) / 8), a.d.kv_heads, a.d.batch), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(prompt_merge_kernel, dim3((uint32_t)((rows + 7) / 8), a.d.kv_heads, a.d.batch), dim3(kMergeThreads), 0, s, a);
   return hipGetLastError();
 }
 

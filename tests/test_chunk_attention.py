@@ -122,6 +122,16 @@ def test_enough_rows_for_one_workgroup_each(batch, tokens):
     run(cfg, [150] * batch, [tokens] * batch, scale=0.2, sequences=[0, batch - 1], heads=[0, cfg.kv_heads - 1])
 
 
+@pytest.mark.parametrize("bits", [2, 4])
+@pytest.mark.parametrize("group_k,group_v", [(32, 32), (64, 64), (128, 128)])
+@pytest.mark.parametrize("paged", [False, True])
+def test_many_sequences_with_few_rows(bits, group_k, group_v, paged):
+    """The units alone fill the device: workgroups of four wavefronts, each a half of a block's codes."""
+    cfg = H.config(1, 64, 8, 4, 512, bits=bits, group_k=group_k, group_v=group_v, residual=40)
+    hist = [450 - 5 * b if b % 3 else 0 for b in range(64)]
+    run(cfg, hist, [1 + b % 31 for b in range(64)], paged, scale=0.2, sequences=[0, 1, 2, 61, 62], heads=[0, 3])
+
+
 @pytest.mark.parametrize("history", [0, 77, 900])
 def test_queries_without_new_tokens_see_the_whole_cache(history):
     cfg = H.config(1, 3, 8, 2, 1024)
