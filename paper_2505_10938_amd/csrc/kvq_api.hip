@@ -851,11 +851,12 @@ bool rows_ok(const void* p, int64_t stride, int64_t heads, int64_t head_dim) {
 
 // How a chunk's attention is dealt: wavefronts of 32 query rows per workgroup, row tiles of a unit, and workgroups that share a
 // row tile's keys.
-//  - Eight wavefronts share what it takes to bring a tile of keys (quantized ones are turned into fp16 rows), four leave less of
-//    a workgroup idle.  Four where the rows of a unit fit them and the units alone fill the device (us, four / eight: 64 sequences x
-//    32 tokens over 4000, 32 / 8 heads 203 / 276; 8 such sequences 51 / 48; 4 x 33 over 8000, 132 rows, 78 / 56; 64 x 60 over 300
-//    75 / 73), and where nothing is quantized and there are at most two rounds of the larger workgroups (prompts of 300 tokens
-//    15 / 18, 1000 30 / 37, 2 x 2000 with 32 kv heads 133 / 143; 4 x 4000 653 / 615, one of 8192 622 / 593).
+//  - Eight wavefronts share what it takes to bring a tile of keys (quantized ones are turned into fp16 rows) and take turns at
+//    the matrix instructions, four leave less of a workgroup idle.  Four where the rows of a unit fit them and there are units
+//    for more than one workgroup per compute unit (us, four / eight: 64 sequences x 32 tokens over 4000, 32 / 8 heads 208 / 264;
+//    256 units, 8 x 128 tokens over 4000 with 32 kv heads, 145 / 134), and where nothing is quantized and there are at most two
+//    rounds of the larger workgroups (prompts of 300 tokens 19.5 / 21.9, 1000 31 / 47, 2 x 2000 with 32 kv heads 118 / 133; 4000
+//    155 / 153).
 //  - A row tile's keys are shared out where there are at most half as many row tiles as compute units, to as many workgroups as
 //    there are compute units, two tiles of 64 keys each at least (4 tokens over 8000, 32 / 8 heads: 193 us with one workgroup each,
 //    36 / 27 / 20 / 28 with 16 / 11 / 4 / 2 tiles each; 33 tokens of 4 sequences 55 with 16 tiles each, 70 with 11).  With more row
@@ -870,7 +871,7 @@ ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quan
   const int64_t units = (int64_t)cfg->batch * cfg->kv_heads, unit_rows = max_tokens * (cfg->q_heads / cfg->kv_heads);
   auto tiles_of = [&](int64_t waves) { return (unit_rows + waves * kvq::kChunkWaveRows - 1) / (waves * kvq::kChunkWaveRows); };
   ChunkShape s;
-  const bool small = tiles_of(4) == 1 && units >= kvq::kComputeUnits;
+  const bool small = tiles_of(4) == 1 && units > kvq::kComputeUnits;
   const bool prompt = n_quant == 0 && units * tiles_of(8) <= 2 * kvq::kComputeUnits;
   s.waves = small || prompt ? 4 : 8;
   s.row_tiles = tiles_of(s.waves);

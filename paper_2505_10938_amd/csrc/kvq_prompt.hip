@@ -4,6 +4,9 @@
 
 #include <type_traits>
 
+// (the parts of the loops are used two or three times each, and called they would keep their registers in memory)
+#define KVQ_INLINE __attribute__((always_inline))
+
 namespace kvq {
 
 namespace {
@@ -138,7 +141,7 @@ __device__ __forceinline__ TileKeys tile_keys(const ChunkArgs& a, const CacheRow
 // One wavefront has 32 query rows, whose products with 64 keys stand transposed in its registers (keys down, one query row
 // per lane and half): the softmax of a row is then work inside a lane, and the weights are, as they stand, an operand of the
 // second product if its keys are taken in the order in which the first one leaves them (16 s + 8 (j / 4) + 4 h + j % 4 for half
-// h of the lanes, element j).  Four wavefronts share the keys' and values' tiles in LDS, two buffers.
+// h of the lanes, element j).  NW wavefronts share the Keys' and Values' tiles in LDS, two buffers of each.
 template <int BITS, int NV, int NW>
 __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs a) {
   constexpr int kRows = NW * kWaveRows;
@@ -198,63 +201,75 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
     for (int r = 0; r < 16; ++r) o[c][r] = 0.0f;
   float m = kNegBig, l = 0.0f;                           // of the lane's row: maximum (log2), sum over the half's keys
 
-  unsigned char* buffer = smem;
-  auto other = [&](unsigned char* p) { return smem + (p == smem ? kBytesBuffer : 0); };
+  auto buffer = [&](int i) { return smem + (i & 1) * kBytesBuffer; };
+  float scale = a.scale, one = 1.0f;
+  asm volatile("" : "+v"(scale), "+v"(one));             // (in registers: read anew, every step would wait for the scale)
 
-  // First product, softmax, second product of one tile.  V stands as rows of channels (two transposing reads bring four keys
-  // each of a channel to a lane) or, dequantized, already by channel in the order of the second product.  `hide(x)` sets the
-  // scores of keys that a row does not see to -infinity, `keep(p)` may look at the weights.  `ask()` may ask for the next tile
-  // between the first product's matrix instructions, `put(s)` store a quarter of it into the other buffer behind each quarter
-  // of the second product.  (That is for quantized tiles, which take instructions to store: 16 sequences of different lengths,
-  // 4-bit codes, 430 us with all of it behind the tile and a wavefront either Keys or Values, 345 so.  With fp16 rows it is even.)
-  auto compute = [&](auto quantized, const unsigned char* buf, auto ask, auto hide, auto keep, auto put) {
-    constexpr bool QUANT = decltype(quantized)::value;
-    const unsigned char* sk = buf + col * kPitchK + 16 * half;
+  // V stands as rows of channels (two transposing reads bring four keys each of a channel to a lane) or, dequantized, already by
+  // channel in the order of the second product.
+  auto value = [&](auto quantized, const unsigned char* buf, int s, int c) KVQ_INLINE -> half8 {
     const unsigned char* sv = buf + kBytesK;
-    auto value = [&](int s, int c) -> half8 {
-      if (QUANT) return *(const half8*)(sv + (32 * c + col) * kPitchT + 32 * s + 16 * half);
-      const unsigned char* at = sv + (16 * s + 4 * half + ((lane & 15) >> 2)) * kPitchV + 2 * (32 * c + (lane & 16) + 4 * (lane & 3));
-      const half4 lo = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_half4_ptr)at));
-      const half4 hi = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_half4_ptr)(at + 8 * kPitchV)));
-      return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-    };
-    // A compute unit has two workgroups, a SIMD a wavefront of each.  The one that has matrix instructions to issue goes first,
-    // so that the other's softmax fills the gaps (8192 tokens, 32 heads: 668 us with no or 695 with the other order, 641 so).
-    // (Eight operands on their way ahead of the matrix instructions, and the first four of the second product's: left to
-    // itself the compiler asks for two at a time and waits for them.)
-    float16v x[2];
-    half8 k[16], v0[4];
+    if constexpr (decltype(quantized)::value) return *(const half8*)(sv + (32 * c + col) * kPitchT + 32 * s + 16 * half);
+    const unsigned char* at = sv + (16 * s + 4 * half + ((lane & 15) >> 2)) * kPitchV + 2 * (32 * c + (lane & 16) + 4 * (lane & 3));
+    const half4 lo = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_half4_ptr)at));
+    const half4 hi = __builtin_bit_cast(half4, __builtin_amdgcn_ds_read_tr16_b64_v4f16((lds_half4_ptr)(at + 8 * kPitchV)));
+    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  // The first product with the Keys in `kb` (scores to x) and the second one with the Values in `vb` (of the weights w): FIRST,
+  // SECOND: which of the two.  Eight operands are on their way ahead of the matrix instructions: left to itself the compiler
+  // asks for two at a time and waits for them.  Of a SIMD's two wavefronts the one that multiplies goes first, it needs few of
+  // the turns (8192 tokens, 32 heads: 577 us, 617 with no order; 45 tokens over 32768 92, 101).
+  float16v x[2];
+  half8 w[4];
+  auto multiply = [&](auto quantized, auto first, auto second, const unsigned char* kb, const unsigned char* vb) KVQ_INLINE {
+    constexpr bool QUANT = decltype(quantized)::value, FIRST = decltype(first)::value, SECOND = decltype(second)::value;
+    const unsigned char* sk = kb + col * kPitchK + 16 * half;
+    __builtin_amdgcn_s_setprio(1);
+    if (FIRST) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) x[0][r] = x[1][r] = 0.0f;
+      for (int r = 0; r < 16; ++r) x[0][r] = x[1][r] = 0.0f;
 #pragma unroll
-    for (int s = 0; s < 8; ++s)
+      for (int s = 0; s < 8; ++s)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) k[2 * s + t] = *(const half8*)(sk + 32 * t * kPitchK + 32 * s);
-    ask();
-#pragma unroll
-    for (int s = 0; s < 8; ++s)
-#pragma unroll
-      for (int t = 0; t < 2; ++t) x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(k[2 * s + t], q[s], x[t], 0, 0, 0);
-#pragma unroll
-    for (int c = 0; c < 4; ++c) v0[c] = value(0, c);
-    __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        for (int t = 0; t < 2; ++t)
+          x[t] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const half8*)(sk + 32 * t * kPitchK + 32 * s), q[s], x[t], 0, 0, 0);
     }
+    if (SECOND) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (i == 4) __builtin_amdgcn_sched_group_barrier(0x100, QUANT ? 4 : 8, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-      if (QUANT) __builtin_amdgcn_sched_group_barrier(0x020, 2, 0);
+      for (int s = 0; s < 4; ++s)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(value(quantized, vb, s, c), w[s], o[c], 0, 0, 0);
     }
+    constexpr int kReadsV = QUANT ? 1 : 2;
+    __builtin_amdgcn_sched_group_barrier(0x100, FIRST ? 8 : 8 * kReadsV, 0);
+    if constexpr (FIRST) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+    }
+    if constexpr (SECOND) {
+#pragma unroll
+      for (int i = 0; i < (FIRST ? 16 : 8); ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, kReadsV, 0);
+      }
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
     __builtin_amdgcn_s_setprio(0);
+  };
+  // The softmax of a tile's scores: x to weights w, and what the outputs have taken so far to the new maximum.  `hide(x)` sets
+  // the scores of keys that a row does not see to -infinity, `keep(x)` may look at the weights.  The sum is of the weights as
+  // they are used, rounded.  A dot product adds two of them, but waits for the matrix unit (16 of them 80 clocks, beside another
+  // wavefront's matrix instructions 600; 32 multiply-adds 160 and 194).  Where a tile takes no work to store that is what a step
+  // waits for (8192 tokens: 590 us with dot products, 576 so), behind quantized tiles it is not (4 x 512 over 8192: 349, 358).
+  auto softmax = [&](auto quantized, auto hide, auto keep) KVQ_INLINE {
     hide(x);
     float top = largest(x[0][0], x[1][0]);
 #pragma unroll
     for (int r = 1; r < 16; ++r) top = largest(largest(top, x[0][r]), x[1][r]);
-    top = largest(top, other_half(top)) * a.scale;
+    top = largest(top, other_half(top)) * scale;
     if (__any(top > m + kSlack)) {
       const float m_new = fmaxf(m, top);
       const float down = __builtin_amdgcn_exp2f(m - m_new);
@@ -268,26 +283,77 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) x[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], a.scale, -m));
+      for (int r = 0; r < 16; ++r) x[t][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[t][r], scale, -m));
     keep(x);
-    __builtin_amdgcn_s_setprio(1);                       // (see above)
+    float l1 = 0.0f;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      half2v w[4];
+      half2v y[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float2v pair = {x[s >> 1][8 * (s & 1) + 2 * j], x[s >> 1][8 * (s & 1) + 2 * j + 1]};
-        w[j] = __builtin_convertvector(pair, half2v);
-        l = __builtin_amdgcn_fdot2(w[j], half2v{1, 1}, l, false);       // (the sum of the weights as they are used)
+        y[j] = __builtin_convertvector(pair, half2v);
+        if (decltype(quantized)::value) {
+          l = __builtin_amdgcn_fdot2(y[j], half2v{1, 1}, l, false);
+        } else {
+          l = __builtin_fmaf((float)y[j][0], one, l);
+          l1 = __builtin_fmaf((float)y[j][1], one, l1);
+        }
       }
-      const half8 weights = {w[0][0], w[0][1], w[1][0], w[1][1], w[2][0], w[2][1], w[3][0], w[3][1]};
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_f16(s == 0 ? v0[c] : value(s, c), weights, o[c], 0, 0, 0);
-      put(s);
+      w[s] = half8{y[0][0], y[0][1], y[1][0], y[1][1], y[2][0], y[2][1], y[3][0], y[3][1]};
     }
+    l += l1;
   };
-  const auto nothing = [](auto&&...) {};
+  const std::true_type yes;
+  const std::false_type no;
+  const auto nothing = [](auto&&...) KVQ_INLINE {};
+
+  // A run of `count` tiles.  With eight wavefronts a SIMD has two of them, and these take turns: while one multiplies (the first
+  // product of a tile and the second one of the tile before), the other has its softmax and stores its share of tiles to come.
+  // Wavefronts 4 to 7 are half a step behind.  Step t of a wavefront: Keys t and Values t - 1 are multiplied; then Keys t + 1
+  // and Values t (the ones behind: t + 2 and t + 1) are stored where Keys t - 1 and Values t - 2 (t and t - 1) were read last
+  // half a step ago.  `load(j)` asks for Keys j and Values j - 1 (behind the last tile: that one again).
+  // (All eight with the same tile, one step after the other: 45 tokens over 32768 96 us, 88 so; 4 x 512 over 8192 359, 348; 16
+  // sequences of different lengths, 4-bit codes, 296, 257; 8192 tokens 595, 576.  Matrix and vector instructions take about as
+  // long as each other, 1000 to 1300 clocks a tile, and under both the device lowers its clock.)
+  const int behind = NW == 8 ? wave >> 2 : 0;
+  auto work = [&](auto quantized, int count, auto load, auto put_k, auto put_v, auto hide) KVQ_INLINE {
+    load(0);
+    put_k(buffer(0));
+    load(1);
+    __syncthreads();
+    if (behind) {
+      put_k(buffer(1));
+      put_v(buffer(0));
+      load(2);
+      __syncthreads();
+    }
+    auto store = [&](int t) KVQ_INLINE {
+      put_k(buffer(t + 1 + behind));
+      put_v(buffer(t + behind));
+      load(t + 2 + behind);
+      __syncthreads();
+    };
+    if (wave_live) {
+      multiply(quantized, yes, no, buffer(0), nullptr);
+      if (NW == 8) __syncthreads();
+      softmax(quantized, hide, nothing);
+      store(0);
+      for (int t = 1; t < count; ++t) {
+        multiply(quantized, yes, yes, buffer(t), buffer(t - 1));
+        if (NW == 8) __syncthreads();
+        softmax(quantized, hide, nothing);
+        store(t);
+      }
+      multiply(quantized, no, yes, nullptr, buffer(count - 1));
+    } else {
+      for (int t = 0; t < count; ++t) {
+        if (NW == 8) __syncthreads();
+        store(t);
+      }
+    }
+    if (NW == 8 && !behind) __syncthreads();
+  };
 
   // ---- quantized tokens, 64 (two blocks) a tile: each wavefront turns its share of a block's Keys and Values into fp16 rows
   {
@@ -296,50 +362,55 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
     const int r = lane >> 4, m16 = lane & 15, part = wave >> 1;
     constexpr int F = 8 / NW;
     QuantRegs<BITS, NV, F> R;
-    uint32_t mask0 = 0, mask1 = 0;
-    // The page numbers of 64 groups at a time, a lane each: a look into the table for every tile would have the tile's loads
-    // wait for it.
-    int pages = 0, first_group = -64;
-    auto place = [&](int blk) -> GroupPlace {            // (called with ascending blocks)
-      const int group = blk >> d.bpg_shift;
-      if (!d.page_table) return {u, group};
-      if (group - first_group >= 64) {                   // uniform
-        first_group = group;
-        pages = d.page_table[(int64_t)b * d.table_stride + min(group + lane, last >> d.bpg_shift)];
-      }
-      const int page = __builtin_amdgcn_readlane(pages, group - first_group);
-      return {d.plane0 + h, min(max(page, 0), d.n_pages - 1)};
+    // Where the blocks are: their numbers in the unit's or the page plane's run, and their mask words, of 64 blocks at a time, a
+    // lane each (a look into the table for every tile would have the tile's loads wait for it).
+    const int64_t run = d.page_table ? d.plane0 + h : u;
+    const int in_group = (1 << d.bpg_shift) - 1;
+    const int cb = F * part, ct = 2 * F * part;          // first fields
+    const unsigned char* const k_run = a.k_codes + run * d.blocks_per_unit * (512 * BITS) + (BITS == 2 ? 4 * (cb >> 1) : 4 * cb);
+    const unsigned char* const v_run = a.v_codes + run * d.blocks_per_unit * (512 * BITS) + (BITS == 2 ? 4 * (ct >> 1) : 1024 * (ct >> 2) + 4 * (ct & 3));
+    const unsigned char* const km_run = a.k_meta + run * d.groups_per_unit * 512 + 64 * cb;
+    const unsigned char* const vm_run = a.v_meta + run * d.blocks_per_unit * (128 * NV) + 4 * (ct * NV / 8);
+    const uint32_t* const mask_run = a.mask + run * d.blocks_per_unit;
+    int first_block = 0, blocks = 0;
+    uint32_t words = 0;
+    auto look_up = [&](int block) KVQ_INLINE {
+      first_block = block;
+      const int mine = min(block + lane, last), group = mine >> d.bpg_shift;
+      int slot = group;
+      if (d.page_table) slot = min(max(d.page_table[(int64_t)b * d.table_stride + group], 0), d.n_pages - 1);
+      blocks = (slot << d.bpg_shift) + (mine & in_group);
+      words = mask_run[blocks];
     };
-    // Where the wavefront's share of a tile is.
-    const unsigned char* at_k = nullptr;
-    const unsigned char* at_v = nullptr;
-    const unsigned char* at_km = nullptr;
-    const unsigned char* at_vm = nullptr;
-    const uint32_t* at_mask[2] = {nullptr, nullptr};
-    auto find = [&](int tile) {
-      const int b0 = 2 * tile, b1 = min(2 * tile + 1, last);     // (behind the last block: that one again, all of it hidden)
-      const int in_group = (1 << d.bpg_shift) - 1;
-      const GroupPlace g0 = place(b0), g1 = place(b1);
-      const int64_t p0 = g0.row * d.blocks_per_unit + ((int64_t)g0.slot << d.bpg_shift) + (b0 & in_group);
-      const int64_t p1 = g1.row * d.blocks_per_unit + ((int64_t)g1.slot << d.bpg_shift) + (b1 & in_group);
-      const int64_t blk = (wave & 1) ? p1 : p0, group = (wave & 1) ? g1.row * d.groups_per_unit + g1.slot : g0.row * d.groups_per_unit + g0.slot;
-      const int cb = F * part, ct = 2 * F * part;        // first fields
-      at_k = a.k_codes + blk * d.block_bytes + (BITS == 2 ? 4 * (cb >> 1) : 4 * cb);
-      at_v = a.v_codes + blk * d.block_bytes + (BITS == 2 ? 4 * (ct >> 1) : 1024 * (ct >> 2) + 4 * (ct & 3));
-      at_km = a.k_meta + group * 512 + 64 * cb;
-      at_vm = a.v_meta + blk * (128 * NV) + 4 * (ct * NV / 8);
-      at_mask[0] = a.mask + p0;
-      at_mask[1] = a.mask + p1;
-    };
-    auto load = [&]() {
+    // The wavefront's block of the tile whose Keys, and of the one whose Values are asked for; the mask words of that one, and of
+    // those before.
+    int k_block = 0;
+    uint32_t hidden[2], seen1[2] = {0, 0}, seen2[2] = {0, 0};
+    auto load = [&](int j) KVQ_INLINE {
+      const int tile = t_begin + j, at = min(2 * tile, last & ~1);
+      const int v_block = k_block;
+      if (j == 0 || at - first_block >= 64) look_up(at);
+      const int i = at - first_block;
+      k_block = __builtin_amdgcn_readlane(blocks, (wave & 1) && at < last ? i + 1 : i);
+      hidden[0] = behind ? seen2[0] : seen1[0];
+      hidden[1] = behind ? seen2[1] : seen1[1];
+      seen2[0] = seen1[0];
+      seen2[1] = seen1[1];
+      seen1[0] = __builtin_amdgcn_readlane(words, i);
+      seen1[1] = at < last ? __builtin_amdgcn_readlane(words, i + 1) : ~0u;
+      const unsigned char* at_k = k_run + (((uint64_t)(uint32_t)k_block) << (BITS == 2 ? 10 : 11));
+      const unsigned char* at_km = km_run + (((uint64_t)(uint32_t)k_block >> d.bpg_shift) << 9);
 #pragma unroll
       for (int th = 0; th < 2; ++th) load_words(R.k[th], at_k + 16 * lane + (BITS == 2 ? 8 : 1024) * th);
-      load_words(R.v, at_v + 16 * lane);
 #pragma unroll
       for (int e = 0; e < F; ++e) {
         R.k_step[e] = *(const u32x4*)(at_km + 64 * e + 16 * r);
         R.k_zero[e] = *(const u32x4*)(at_km + 64 * e + 16 * r + 256);
       }
+      if (j == 0) return;
+      const unsigned char* at_v = v_run + (((uint64_t)(uint32_t)v_block) << (BITS == 2 ? 10 : 11));
+      const unsigned char* at_vm = vm_run + ((uint64_t)(uint32_t)v_block) * (128 * NV);
+      load_words(R.v, at_v + 16 * lane);
       if constexpr (NV == 1) {
         const u32x4 st = *(const u32x4*)(at_vm + 16 * r), ze = *(const u32x4*)(at_vm + 16 * r + 64);
 #pragma unroll
@@ -354,26 +425,29 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
           load_words(R.v_zero[v], at_vm + 4 * NV * (4 * r + v) + 64 * NV);
         }
       }
-      mask0 = *at_mask[0];                               // (every wavefront wants both blocks' mask words)
-      mask1 = *at_mask[1];
     };
-    // Piece s of the share's 2 F: a field of Keys (8 channels from 32 cb + 8 r on of token 16 th + m16) and one of Values (tokens
-    // 8 r .. of channel 16 ct + m16).
-    auto put_piece = [&](unsigned char* buf, int s) {
-      if (s >= 2 * F) return;
-      const int token0 = 32 * (wave & 1), e = F == 2 ? s & 1 : 0, th = F == 2 ? s >> 1 : s;
-      {
-        uint32_t st[4], ze[4];
+    // A field of Keys: 8 channels from 32 cb + 8 r on of token 16 th + m16.
+    const int token0 = 32 * (wave & 1);
+    auto put_k = [&](unsigned char* buf) KVQ_INLINE {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-          st[v] = R.k_step[e][v];
-          ze[v] = R.k_zero[e][v];
+      for (int th = 0; th < 2; ++th)
+#pragma unroll
+        for (int e = 0; e < F; ++e) {
+          uint32_t st[4], ze[4];
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            st[v] = R.k_step[e][v];
+            ze[v] = R.k_zero[e][v];
+          }
+          const int odd = BITS == 2 ? (F == 2 ? e : part & 1) : 0;
+          *(u32x4*)(buf + (token0 + 16 * th + m16) * kPitchK + 64 * F * part + 64 * e + 16 * r) =
+              dequant_field<BITS>(R.k[th][BITS == 2 ? 0 : e], odd, st, ze);
         }
-        const int odd = BITS == 2 ? (F == 2 ? e : part & 1) : 0;
-        *(u32x4*)(buf + (token0 + 16 * th + m16) * kPitchK + 64 * F * part + 64 * e + 16 * r) =
-            dequant_field<BITS>(R.k[th][BITS == 2 ? 0 : e], odd, st, ze);
-      }
-      {
+    };
+    // A field of Values: tokens 8 r .. of channel 16 (ct + s) + m16.
+    auto put_v = [&](unsigned char* buf) KVQ_INLINE {
+#pragma unroll
+      for (int s = 0; s < 2 * F; ++s) {
         constexpr int kOf = F == 2 ? 1 : 0;
         uint32_t st[4], ze[4];
 #pragma unroll
@@ -381,18 +455,13 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
           st[v] = R.v_step[v][NV == 4 && kOf ? s >> 1 : 0];
           ze[v] = R.v_zero[v][NV == 4 && kOf ? s >> 1 : 0];
         }
-        const u32x4 x = dequant_field<BITS>(R.v[BITS == 2 ? s >> 1 : s], BITS == 2 ? s & 1 : 0, st, ze);
+        const u32x4 y = dequant_field<BITS>(R.v[BITS == 2 ? s >> 1 : s], BITS == 2 ? s & 1 : 0, st, ze);
         unsigned char* sv = buf + kBytesK + (32 * F * part + 16 * s + m16) * kPitchT + 2 * (token0 + 16 * (r >> 1) + 4 * (r & 1));
-        *(u32x2*)sv = u32x2{x[0], x[1]};
-        *(u32x2*)(sv + 16) = u32x2{x[2], x[3]};
+        *(u32x2*)sv = u32x2{y[0], y[1]};
+        *(u32x2*)(sv + 16) = u32x2{y[2], y[3]};
       }
     };
-    auto put_all = [&](unsigned char* buf) {
-#pragma unroll
-      for (int s = 0; s < 2 * F; ++s) put_piece(buf, s);
-    };
-    uint32_t hidden[2];
-    auto hide = [&](float16v (&x)[2]) {
+    auto hide = [&](float16v (&x)[2]) KVQ_INLINE {
       if (hidden[0] | hidden[1]) {                       // uniform
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -403,45 +472,20 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
         }
       }
     };
-    // (the words are looked at when the tile is, not when they are asked for: everything would wait for them)
-    auto look = [&](int tile) {
-      hidden[0] = __builtin_amdgcn_readfirstlane(mask0);
-      hidden[1] = 2 * tile + 1 > last ? ~0u : (uint32_t)__builtin_amdgcn_readfirstlane(mask1);
-    };
-    if (t_begin < qe) {
-      find(t_begin);
-      load();
-      put_all(buffer);
-      look(t_begin);
-      __syncthreads();
-      for (int t = t_begin; t + 1 < qe; ++t) {
-        find(t + 1);
-        unsigned char* next = other(buffer);
-        if (wave_live) {
-          compute(std::true_type{}, buffer, load, hide, nothing, [&](int s) { put_piece(next, s); });
-        } else {
-          load();
-          put_all(next);
-        }
-        look(t + 1);
-        buffer = next;
-        __syncthreads();
-      }
-      if (wave_live) compute(std::true_type{}, buffer, nothing, hide, nothing, nothing);
-      buffer = other(buffer);
-    }
+    if (t_begin < qe) work(yes, qe - t_begin, load, put_k, put_v, hide);
   }
 
   // ---- full-precision rows, 64 a tile
   const int piece = tid & 15, line = tid >> 4;
   constexpr int kPasses = 16 / NW, kLines = 4 * NW;      // rows of a tile: kLines at a time
   u32x4 rk[kPasses], rv[kPasses];
-  auto store = [&](unsigned char* buf) {
+  auto put_k = [&](unsigned char* buf) KVQ_INLINE {
 #pragma unroll
-    for (int i = 0; i < kPasses; ++i) {
-      *(u32x4*)(buf + (kLines * i + line) * kPitchK + 16 * piece) = rk[i];
-      *(u32x4*)(buf + kBytesK + (kLines * i + line) * kPitchV + 16 * piece) = rv[i];
-    }
+    for (int i = 0; i < kPasses; ++i) *(u32x4*)(buf + (kLines * i + line) * kPitchK + 16 * piece) = rk[i];
+  };
+  auto put_v = [&](unsigned char* buf) KVQ_INLINE {
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) *(u32x4*)(buf + kBytesK + (kLines * i + line) * kPitchV + 16 * piece) = rv[i];
   };
 
   // new tokens that all of the workgroup's rows see
@@ -449,29 +493,19 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
     const int nb = max(t_begin, tq), ne = min(t_end, tq + ti);
     if (nb < ne) {
       const uint32_t row_bytes = (uint32_t)a.kv_stride * 2, offset = line * row_bytes + 16 * piece;
-      const int64_t first = s0 * a.kv_stride + h * kHeadDim;
-      auto load = [&](int tile) {
-        const int64_t at = 2 * (first + (int64_t)(tile - tq) * kTile * a.kv_stride);       // (uniform)
-        const unsigned char* pk = (const unsigned char*)a.k_new + at;
-        const unsigned char* pv = (const unsigned char*)a.v_new + at;
+      const int64_t first = s0 * a.kv_stride + h * kHeadDim + (int64_t)(nb - tq) * kTile * a.kv_stride;
+      const int count = ne - nb;
+      const unsigned char* at_k = (const unsigned char*)(a.k_new + first);
+      const unsigned char* at_v = (const unsigned char*)(a.v_new + first);
+      auto rows = [&](u32x4 (&x)[kPasses], const unsigned char*& at, bool more) KVQ_INLINE {
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-          rk[i] = *(const u32x4*)(pk + (offset + kLines * i * row_bytes));
-          rv[i] = *(const u32x4*)(pv + (offset + kLines * i * row_bytes));
-        }
+        for (int i = 0; i < kPasses; ++i) x[i] = *(const u32x4*)(at + (offset + kLines * i * row_bytes));
+        at += more ? row_bytes * kTile : 0;              // (uniform)
       };
-      load(nb);
-      store(buffer);
-      __syncthreads();
-      for (int t = nb; t + 1 < ne; ++t) {
-        load(t + 1);
-        if (wave_live) compute(std::false_type{}, buffer, nothing, nothing, nothing, nothing);
-        buffer = other(buffer);
-        store(buffer);
-        __syncthreads();
-      }
-      if (wave_live) compute(std::false_type{}, buffer, nothing, nothing, nothing, nothing);
-      buffer = other(buffer);
+      work(no, count, [&](int j) KVQ_INLINE {
+        rows(rk, at_k, j + 1 < count);
+        if (j > 0) rows(rv, at_v, j < count);
+      }, put_k, put_v, nothing);
     }
   }
 
@@ -486,7 +520,7 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
     const __half* nv = a.v_new + s0 * a.kv_stride + h * kHeadDim + 8 * piece;
     // Where some rows see a new token and others do not, its Value must not reach the others, for 0 times an infinity is a
     // NaN: what is not finite is left out of the tile (and counted in by `late` for the rows that see it).
-    auto load = [&](int tile) -> bool {
+    auto load = [&](int tile) KVQ_INLINE -> bool {
       const bool own = tile >= rows_end;                 // uniform
       const int first = own ? (tile - rows_end + ti) * kTile : (tile - tq - ti) * kTile;
 #pragma unroll
@@ -555,8 +589,10 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
       }
     };
     if (fb < t_end) {
+      if (t_begin < fb) __syncthreads();                 // (the last tile's Values)
       bool odd = load(fb) && sort_out();
-      store(buffer);
+      put_k(buffer(fb));
+      put_v(buffer(fb));
       odd = __syncthreads_or(odd);
       for (int t = fb; t < t_end; ++t) {
         const bool more = t + 1 < t_end;
@@ -568,21 +604,23 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
         const int limit = (own ? min(n_new, token + 1) : n_rows) - base;
         const int most = (own ? min(n_new, ((wave_row + kWaveRows - 1) >> a.g_shift) + 1) : n_rows) - base;
         if (wave_live && most > 0) {
-          compute(std::false_type{}, buffer, nothing, [&](float16v (&x)[2]) {
+          multiply(no, yes, no, buffer(t), nullptr);
+          softmax(no, [&](float16v (&x)[2]) KVQ_INLINE {
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
               for (int r = 0; r < 16; ++r)
                 if (32 * i + 8 * (r >> 2) + (r & 3) + 4 * half >= limit) x[i][r] = -__builtin_inff();
-          }, [&](float16v (&x)[2]) {
-            if (odd) late(t, limit, (float*)(other(buffer) + wave * (kWaveRows * 32 * 4)), x);     // (uniform)
-          }, nothing);
+          }, [&](float16v (&x)[2]) KVQ_INLINE {
+            if (odd) late(t, limit, (float*)(buffer(t + 1) + wave * (kWaveRows * 32 * 4)), x);     // (uniform)
+          });
+          multiply(no, no, yes, nullptr, buffer(t));
         }
-        buffer = other(buffer);
         if (more) {
           if (odd) __syncthreads();                      // (the weights' place in the other buffer)
           odd = next_own && sort_out();
-          store(buffer);
+          put_k(buffer(t + 1));
+          put_v(buffer(t + 1));
           odd = __syncthreads_or(odd);
         }
       }
