@@ -167,6 +167,7 @@ struct ChunkArgs {
   int32_t splits;                       // by so many workgroups at most
   int32_t parts;                        // 1, 2, 4 or 8: units * parts is a multiple of 8
   int32_t part_tiles;                   // row tiles of a part of a unit, rounded up
+  int32_t ranked;                       // sequences in the order of their work rather than of their numbers
   float* share_ml;                      // splits > 1: [unit][row][split][2] maximum (log2) and sum of a row's share
   float* share_o;                       //             [unit][row][split][head_dim]
 };
