@@ -533,7 +533,9 @@ int32_t kvq_decode_attention_planned(const kvq_config* cfg, int32_t layer, const
  *                sequence b's from row b * max_tokens on; total is batch * max_tokens then
  *   total      : rows of the packed arrays, 1 .. 2^31 - 1
  *   max_tokens : upper bound of the tokens of one sequence, 1 .. total (sizes the launches; of a longer sequence the
- *                first max_tokens tokens are taken)
+ *                first max_tokens tokens are taken).  KVQ_ERR_UNSUPPORTED for what a launch cannot number: in
+ *                kvq_prompt_attention above 2^30 query rows of a kv head (max_tokens * q_heads / kv_heads) or 2^23 workgroups,
+ *                of 128 rows each at least; in kvq_extend from 2^22 groups of group_k tokens on, of all sequences and kv heads
  * The kernels clamp starts to [0, total], so a corrupt array gives wrong results, no access outside the arrays.  Rows
  * that belong to no sequence are neither read nor written.
  */
@@ -549,10 +551,10 @@ typedef struct kvq_chunk {
  * tokens up to the query's own, in full precision: Method, prefill phase).  On an empty cache this is the attention of
  * a prompt.  The cache is read only and the new rows join it nowhere (kvq_extend does that).
  *   q          : device fp16, token i of the packed array at element offset i * q_stride, its q_heads rows of head_dim
- *                behind each other; 16-byte aligned; q_stride >= q_heads * head_dim, a multiple of 8
+ *                behind each other; 16-byte aligned; q_stride >= q_heads * head_dim, a multiple of 8, at most 2^23
  *   k_new, v_new : device fp16, token i's kv_heads rows at element offset i * kv_stride; 16-byte aligned; kv_stride >=
- *                kv_heads * head_dim, a multiple of 8, at most 2^23 (as q_stride).  (q, k_new and v_new may be parts of one projection's output.)
- *                Both NULL: no new tokens, every query sees the whole cache and nothing else (cross attention to an
+ *                kv_heads * head_dim, a multiple of 8, at most 2^23.  (q, k_new and v_new may be parts of one projection's
+ *                output.)  Both NULL: no new tokens, every query sees the whole cache and nothing else (cross attention to an
  *                encoder's states); kv_stride is ignored
  *   seq_state  : as in kvq_decode_attention_ragged, with n_quant and n_res upper bounds of the sequences' (longer ones
  *                are truncated to them) and res_start ignored; `active` plays no part.  NULL: n_quant, res_start and n_res are
@@ -568,7 +570,8 @@ typedef struct kvq_chunk {
  *                of queries that see it infinite or NaN).  New tokens behind a query's own may hold anything: they do not
  *                change its output
  *   Rounding   : the dequantized rows and the softmax weights are rounded to fp16 for the matrix products, which, like
- *                the softmax's maxima and sums, are fp32
+ *                the softmax's maxima and sums, are fp32.  (The decode step's calls keep the dequantized rows in 32 bits.
+ *                Keys of normal magnitude with channels six times as large: outputs 6e-4 off in the root mean square, 2e-4 there)
  */
 int64_t kvq_prompt_workspace_bytes(const kvq_config* cfg, int32_t max_tokens, int32_t n_quant, int32_t n_res);
 int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q, int64_t q_stride, const void* k_new,
@@ -587,7 +590,8 @@ int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q
  *                is not one that these calls produce, or whose groups do not fit max_seq, is left alone by both calls.
  *                NULL: the three numbers are every sequence's state, n_res < R + G, res_start a multiple of group_k, and the
  *                groups have to fit (KVQ_ERR_INVALID_ARG); the caller then counts on for itself: n_quant + groups * G,
- *                (res_start + groups * G) mod res_rows, n_res + n - groups * G
+ *                (res_start + groups * G) mod res_rows, n_res + n - groups * G.  (With `starts` the groups that a sequence
+ *                would need are known on the device only: one whose do not fit is left alone there)
  *   selected   : device uint8 scratch of at least batch * kv_heads * G * ((max_tokens + G - 1) / G) bytes
  *                (KVQ_ERR_WORKSPACE below), contents unspecified on return
  *   qcache     : dense or paged; the table's entries of the new groups must be in place
@@ -662,7 +666,7 @@ int32_t kvq_compact_pages(const kvq_config* cfg, kvq_qcache from, const int32_t*
  *   axes       : 1 .. 8
  *   pair_axis  : HOST uint8 [head_dim / 2], each below axes (it may go when the call returns)
  *   freq       : device fp32 [head_dim / 2], 4-byte aligned: radians per position, finite
- *   tokens     : 1 .. 2^31 - 1
+ *   tokens     : 1 .. 2^26 - 64 (KVQ_ERR_UNSUPPORTED above)
  *
  * kvq_rope_axes : rows of `tokens` tokens: their q_heads query rows and their kv_heads Key rows.
  *   q, k       : device fp16, 16-byte aligned, token i at element offset i * q_stride (k_stride); strides as in

@@ -435,6 +435,12 @@ class KVCache:
         if self.page_table is None:
             raise ValueError("the cache has no pages")
 
+    def _pool(self, to, table=True):
+        """`to` has to be laid out as the cache's own pool is."""
+        names = ("layers", "kv_heads", "head_dim", "bits", "group_k", "group_v") + (("batch", "max_seq") if table else ())
+        if any(getattr(to.cfg, n) != getattr(self.cfg, n) for n in names) or to.k_codes.device != self.k_codes.device:
+            raise ValueError("the pool is of another configuration, or on another device")
+
     def free_pages(self, stream=None):
         """The pages that no quantized group of any sequence lies in: (int32 [n_pages], ascending, then -1; int32 [2]: free
         pages, live pages), both on the device."""
@@ -452,6 +458,8 @@ class KVCache:
         None: of the same pool)."""
         self._paged()
         self._pairs(pairs)
+        if to is not None:
+            self._pool(to, table=False)
         if pairs.shape[0] == 0:
             return
         self._behind_prompts(stream)
@@ -465,6 +473,7 @@ class KVCache:
         self._paged()
         if to.k_codes.data_ptr() == self.k_codes.data_ptr():
             raise ValueError("a pool is not compacted into itself")
+        self._pool(to)
         self._behind_prompts(stream)
         seq_state, state = self._sequences()
         with self._launching(stream):
@@ -478,6 +487,7 @@ class KVCache:
         """The arrays and the table of a PagePool become the cache's (those that it had are given back with the last
         reference to them: calls that still use them have to be on the current stream, or through)."""
         self._paged()
+        self._pool(pool)
         for name in ("k_codes", "k_meta", "v_codes", "v_meta", "mask", "page_table", "n_pages"):
             setattr(self, name, getattr(pool, name))
         self._bind()

@@ -132,6 +132,16 @@ def test_many_sequences_with_few_rows(bits, group_k, group_v, paged):
     run(cfg, hist, [1 + b % 31 for b in range(64)], paged, scale=0.2, sequences=[0, 1, 2, 61, 62], heads=[0, 3])
 
 
+@pytest.mark.parametrize("batch,kv_heads,most", [(40, 16, 40), (24, 16, 300), (64, 24, 3)])
+def test_many_sequences_of_different_lengths(batch, kv_heads, most):
+    """More workgroups than the device takes at once, dealt by the sequences' work."""
+    cfg = H.config(1, batch, kv_heads, kv_heads, 512, residual=40)
+    g = np.random.default_rng(batch)
+    hist, new = g.integers(0, 500, batch), np.minimum(g.integers(0, 2 * most, batch), most)
+    hist[:2], new[:3], new[5] = (0, 499), (most, 1, 0), 0
+    run(cfg, hist.tolist(), new.tolist(), paged=True, heads=[0, 7])
+
+
 @pytest.mark.parametrize("history", [0, 77, 900])
 def test_queries_without_new_tokens_see_the_whole_cache(history):
     cfg = H.config(1, 3, 8, 2, 1024)

@@ -186,3 +186,23 @@ def test_arguments_of_the_methods():
             print("not refused:", i)
     with pytest.raises(B.KvqError):
         cache.rope_rows(torch.zeros(3, dtype=torch.int32), torch.zeros(64), [0] * 63)
+
+
+def test_pools_of_another_configuration():
+    c = KC.make_config(2, 2, 8, 2, 512)
+    cache = KC.KVCache(c, device="cpu", n_pages=20)
+    pairs = torch.zeros(1, 2, dtype=torch.int32)
+    for other in (KC.make_config(1, 2, 8, 2, 512), KC.make_config(2, 2, 8, 4, 512), KC.make_config(2, 2, 8, 2, 512, bits=4),
+                  KC.make_config(2, 2, 8, 2, 512, group_k=64), KC.make_config(2, 2, 8, 2, 512, group_v=64)):
+        to = KC.PagePool(other, 30, device="cpu")
+        for call in (lambda: cache.compact_into(to), lambda: cache.adopt(to), lambda: cache.copy_pages(pairs, to)):
+            with pytest.raises(ValueError):
+                call()
+    for other in (KC.make_config(2, 3, 8, 2, 512), KC.make_config(2, 2, 8, 2, 1024)):   # (the tables differ, the pages do not)
+        to = KC.PagePool(other, 30, device="cpu")
+        for call in (lambda: cache.compact_into(to), lambda: cache.adopt(to)):
+            with pytest.raises(ValueError):
+                call()
+    same = KC.PagePool(c, 30, device="cpu")
+    cache.adopt(same)
+    assert cache.n_pages == 30 and cache.page_table is same.page_table
