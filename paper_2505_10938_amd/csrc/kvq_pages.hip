@@ -33,7 +33,7 @@ struct ForkArgs {
   Dims d;
   const int32_t* pairs;
   int32_t n_pairs;
-  int32_t slice;             // elements of a unit that one block has
+  int32_t slice_shift;       // 1 << slice_shift elements of a unit are one block's
   const int32_t* seq;
   int32_t n_quant, res_start, n_res;
   const int32_t* pool_count;
@@ -56,13 +56,17 @@ __device__ __forceinline__ Live live_of(const ForkArgs& a, int b) {
   return s;
 }
 
+// UNIFORM: a wavefront's elements are of one pair (slices of 64 and more), which is then looked up by the scalar unit.  (32 layers, 8 of 32
+// sequences take over others, 335 MB: 94 us with slices of any length, a division per element, and lookups by the lanes, 65 so.)
+template <bool UNIFORM>
 __global__ void __launch_bounds__(kForkThreads) fork_kernel(ForkArgs a) {
   const Dims& d = a.d;
+  const int in_slice = (1 << a.slice_shift) - 1, group_shift = 5 + d.bpg_shift;
   int j = 0;
   while (j + 1 < a.n_jobs && blockIdx.x >= a.job[j + 1].first_block) ++j;
   const ForkJob job = a.job[j];
   const uint32_t at = blockIdx.x - job.first_block;
-  const int plane = at / job.slices, e0 = (at - plane * job.slices) * a.slice;
+  const int plane = at / job.slices, e0 = (at - plane * job.slices) << a.slice_shift;
   const int layer = plane / d.kv_heads, h = plane - layer * d.kv_heads;
   auto unit_of = [&](int b) -> int64_t {
     return job.kind == kTable ? b : ((int64_t)layer * d.batch + b) * d.kv_heads + h;
@@ -72,7 +76,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(ForkArgs a) {
 #pragma unroll
   for (int k = 0; k < kForkLoads; ++k) {
     const int i = k * kForkThreads + threadIdx.x;
-    const int p = i / a.slice, e = e0 + (i - p * a.slice);
+    const int p = UNIFORM ? __builtin_amdgcn_readfirstlane(i >> a.slice_shift) : i >> a.slice_shift, e = e0 + (i & in_slice);
     to[k] = -1;
     v[k] = u32x4{0, 0, 0, 0};
     if (p >= a.n_pairs || e >= job.elems) continue;
@@ -86,9 +90,9 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(ForkArgs a) {
       rel += rel < 0 ? d.res_rows : 0;
       live = rel < s.nr;
     } else if (job.kind == kGroups) {
-      live = e < live_of(a, src).nq / d.G * job.per_group;
+      live = e < (live_of(a, src).nq >> group_shift) * job.per_group;
     } else if (job.kind == kTable) {
-      live = e < live_of(a, src).nq / d.G;
+      live = e < live_of(a, src).nq >> group_shift;
     } else {
       const int slot = job.kind == kPoolRows ? e >> 4 : job.kind == kPoolPairs ? e >> 1 : e;
       live = slot < d.N ? slot < a.pool_count[u] : slot - d.N < a.aux_count[u];
@@ -105,7 +109,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(ForkArgs a) {
   for (int k = 0; k < kForkLoads; ++k) {
     if (to[k] < 0) continue;
     const int i = k * kForkThreads + threadIdx.x;
-    const int e = e0 + (i - i / a.slice * a.slice);
+    const int e = e0 + (i & in_slice);
     unsigned char* p = (unsigned char*)job.base + unit_of(to[k]) * job.unit_stride;
     if (job.wide) ((u32x4*)p)[e] = v[k];
     else ((uint32_t*)p)[e] = v[k][0];
@@ -334,7 +338,9 @@ hipError_t launch_fork(const Dims& d, int32_t layers, const int32_t* pairs, int3
   a.d = d;
   a.pairs = pairs;
   a.n_pairs = n_pairs;
-  a.slice = kForkItems / n_pairs;
+  a.slice_shift = 0;
+  while ((n_pairs << (a.slice_shift + 1)) <= kForkItems) ++a.slice_shift;
+  const int32_t slice = 1 << a.slice_shift;
   a.seq = seq;
   a.n_quant = n_quant;
   a.res_start = res_start;
@@ -353,7 +359,7 @@ hipError_t launch_fork(const Dims& d, int32_t layers, const int32_t* pairs, int3
     j.elems = (int32_t)elems;
     j.per_group = per_group;
     j.first_block = (uint32_t)blocks;
-    j.slices = (int32_t)((elems + a.slice - 1) / a.slice);
+    j.slices = (int32_t)((elems + slice - 1) / slice);
     blocks += (int64_t)j.slices * (kind == kTable ? 1 : planes);
   };
   const int64_t row = kHeadDim * 2;
@@ -378,7 +384,8 @@ hipError_t launch_fork(const Dims& d, int32_t layers, const int32_t* pairs, int3
     job(qc.mask, all * per * 4, kGroups, false, groups * per, (int32_t)per);
   }
   if (blocks > (1 << 24) - 1) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL(fork_kernel, dim3((uint32_t)blocks), dim3(kForkThreads), 0, s, a);
+  const auto kern = slice >= 64 ? fork_kernel<true> : fork_kernel<false>;
+  hipLaunchKernelGGL(kern, dim3((uint32_t)blocks), dim3(kForkThreads), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   hipLaunchKernelGGL(fork_state_kernel, dim3(planes + (seq ? 1 : 0)), dim3(kForkThreads), 0, s, d, pairs, n_pairs, planes, seq,
