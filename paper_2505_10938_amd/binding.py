@@ -457,9 +457,13 @@ def _axes(cfg, pair_axis):
     pairs = cfg.head_dim // 2
     if pair_axis is None:
         return bytes(pairs)
-    if len(pair_axis) != pairs or not all(0 <= int(a) < 256 for a in pair_axis):
+    try:
+        axes = bytes(pair_axis if isinstance(pair_axis, (bytes, list, tuple)) else [int(a) for a in pair_axis])
+    except (TypeError, ValueError):                        # (not numbers, or not in 0 .. 255)
+        axes = b""
+    if len(axes) != pairs:
         raise KvqError(KVQ_ERR_INVALID_ARG, "pair_axis")
-    return bytes(int(a) for a in pair_axis)
+    return axes
 
 
 def kvq_rope_axes(cfg, q, q_stride, k, k_stride, tokens, positions, axes, pair_axis, freq, q_out, q_out_stride, k_out,

@@ -32,15 +32,20 @@ def _on(stream, device):
     return torch.cuda.stream(stream)
 
 
+_NOTHING = contextlib.nullcontext()
+
+
 def _token_rows(t, heads, head_dim):
     """A packed array of tokens, [..., heads, head_dim] fp16 with rows of a token behind each other, as (tensor, tokens,
     elements from token to token)."""
-    if t.dtype != torch.float16 or t.dim() < 3 or tuple(t.shape[-2:]) != (heads, head_dim):
-        raise ValueError(f"fp16 [..., {heads}, {head_dim}] is wanted, not {t.dtype} {tuple(t.shape)}")
-    rows = t.view(-1, heads, head_dim)                     # (a RuntimeError if the tokens are not evenly spaced)
-    if rows.shape[0] == 0 or (heads > 1 and rows.stride(1) != head_dim) or rows.stride(2) != 1:
+    shape = t.shape
+    if t.dtype is not torch.float16 or len(shape) < 3 or shape[-2] != heads or shape[-1] != head_dim:
+        raise ValueError(f"fp16 [..., {heads}, {head_dim}] is wanted, not {t.dtype} {tuple(shape)}")
+    rows = t if len(shape) == 3 else t.view(-1, heads, head_dim)     # (a RuntimeError if the tokens are not evenly spaced)
+    n, (token, head, channel) = rows.shape[0], rows.stride()
+    if n == 0 or (heads > 1 and head != head_dim) or channel != 1:
         raise ValueError("a token's heads have to lie behind each other, and there has to be one token at least")
-    return rows, rows.shape[0], rows.stride(0) if rows.shape[0] > 1 else heads * head_dim
+    return rows, n, token if n > 1 else heads * head_dim
 
 
 class PagePool:
@@ -300,7 +305,10 @@ class KVCache:
         """Context in which a call's tensors belong to `stream` (None: the current one) of the cache's device."""
         if stream is not None:
             return _on(stream, self.device)
-        return torch.cuda.device(self.device) if self.device.type == "cuda" else contextlib.nullcontext()
+        device = self.device
+        if device.type != "cuda" or device.index is None or device.index == torch.cuda.current_device():
+            return _NOTHING                                # (entering the device that is current costs 1.5 us)
+        return torch.cuda.device(device)
 
     def _attend(self, layer, q, k_new, v_new, starts, max_tokens, seq_state, state, out, stream):
         cfg = self.cfg
@@ -315,7 +323,7 @@ class KVCache:
         self._behind_prompts(stream)
         with self._launching(stream):
             if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
             elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
                 raise ValueError("the output is fp16, contiguous, of the queries' shape")
             n_quant, res_start, n_res = state
@@ -377,7 +385,7 @@ class KVCache:
                     args.append((None, 0, None, 0))
                     continue
                 if out is None:
-                    out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+                    out = torch.empty_like(x, memory_format=torch.contiguous_format)
                 (rows, n, stride), (to, m, to_stride) = (_token_rows(t, heads, cfg.head_dim) for t in (x, out))
                 if n != tokens or m != tokens:
                     raise ValueError("there has to be a position for every token, and an output")
@@ -438,7 +446,8 @@ class KVCache:
     def _pool(self, to, table=True):
         """`to` has to be laid out as the cache's own pool is."""
         names = ("layers", "kv_heads", "head_dim", "bits", "group_k", "group_v") + (("batch", "max_seq") if table else ())
-        if any(getattr(to.cfg, n) != getattr(self.cfg, n) for n in names) or to.k_codes.device != self.k_codes.device:
+        same = to.cfg is self.cfg or all(getattr(to.cfg, n) == getattr(self.cfg, n) for n in names)
+        if not same or to.k_codes.device != self.k_codes.device:
             raise ValueError("the pool is of another configuration, or on another device")
 
     def free_pages(self, stream=None):
