@@ -571,7 +571,8 @@ typedef struct kvq_chunk {
  *                change its output
  *   Rounding   : the dequantized rows and the softmax weights are rounded to fp16 for the matrix products, which, like
  *                the softmax's maxima and sums, are fp32.  (The decode step's calls keep the dequantized rows in 32 bits.
- *                Keys of normal magnitude with channels six times as large: outputs 6e-4 off in the root mean square, 2e-4 there)
+ *                Keys of normal magnitude with channels six times as large: outputs 5e-4 to 8e-4 off in the root mean square,
+ *                2e-4 there)
  */
 int64_t kvq_prompt_workspace_bytes(const kvq_config* cfg, int32_t max_tokens, int32_t n_quant, int32_t n_res);
 int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q, int64_t q_stride, const void* k_new,
