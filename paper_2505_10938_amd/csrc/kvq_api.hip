@@ -852,11 +852,13 @@ bool rows_ok(const void* p, int64_t stride, int64_t heads, int64_t head_dim) {
 // How a chunk's attention is dealt: wavefronts of 32 query rows per workgroup, row tiles of a unit, and workgroups that share a
 // row tile's keys.
 //  - Eight wavefronts share what it takes to bring a tile of keys (quantized ones are turned into fp16 rows) and take turns at
-//    the matrix instructions, four leave less of a workgroup idle.  Four where the rows of a unit fit them and there are units
-//    for more than one workgroup per compute unit (us, four / eight: 64 sequences x 32 tokens over 4000, 32 / 8 heads 208 / 264;
-//    256 units, 8 x 128 tokens over 4000 with 32 kv heads, 145 / 134), and where nothing is quantized and there are at most two
-//    rounds of the larger workgroups (prompts of 300 tokens 19.5 / 21.9, 1000 31 / 47, 2 x 2000 with 32 kv heads 118 / 133; 4000
-//    155 / 153).
+//    the matrix instructions, four leave less of a workgroup idle, and two such workgroups fit a compute unit.  Four where the
+//    rows of a unit fit them and there are workgroups for that: more units than compute units (us, four / eight: 64
+//    sequences x 32 tokens over 4000, 32 / 8 heads 208 / 264), or more than a quarter as many with keys to share out among two
+//    workgroups per compute unit (tokens over 4000, 32 kv heads: 3 x 5 44 / 78, 4 x 32 48 / 63, 8 x 5 76 / 102, 8 x 128 133 /
+//    138, 2 x 5, 64 units, 33 / 37; 8 kv heads: 24 x 16 over 2000 62 / 66, 8 x 16, 64 units, 44 / 43; over 700, 15 tiles, 24 x
+//    20 42 / 36); and where nothing is quantized and there are at most two rounds of the larger workgroups (prompts of 300
+//    tokens 19.5 / 21.9, 1000 31 / 47, 2 x 2000 with 32 kv heads 118 / 133; 4000 155 / 153).
 //  - A row tile's keys are shared out where there are at most half as many row tiles as compute units, to as many workgroups as
 //    there are compute units, two tiles of 64 keys each at least (4 tokens over 8000, 32 / 8 heads: 193 us with one workgroup each,
 //    36 / 27 / 20 / 28 with 16 / 11 / 4 / 2 tiles each; 33 tokens of 4 sequences 55 with 16 tiles each, 70 with 11).  With more row
@@ -871,15 +873,19 @@ ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quan
   const int64_t units = (int64_t)cfg->batch * cfg->kv_heads, unit_rows = max_tokens * (cfg->q_heads / cfg->kv_heads);
   auto tiles_of = [&](int64_t waves) { return (unit_rows + waves * kvq::kChunkWaveRows - 1) / (waves * kvq::kChunkWaveRows); };
   ChunkShape s;
-  const bool small = tiles_of(4) == 1 && units > kvq::kComputeUnits;
   const bool prompt = n_quant == 0 && units * tiles_of(8) <= 2 * kvq::kComputeUnits;
-  s.waves = small || prompt ? 4 : 8;
-  s.row_tiles = tiles_of(s.waves);
   const int64_t fp_rows = n_res + cfg->outlier_budget + cfg->aux_capacity;
   const int64_t held = (n_quant + 63) / 64 + (fp_rows + 63) / 64, own = with_new ? (max_tokens + 63) / 64 : 0;
   const int64_t longest = held + own;
+  const bool shared = units > kvq::kComputeUnits / 4 && units <= kvq::kComputeUnits && longest >= 24;
+  const bool small = tiles_of(4) == 1 && (units > kvq::kComputeUnits || shared);
+  s.waves = small || prompt ? 4 : 8;
+  s.row_tiles = tiles_of(s.waves);
   s.most = longest > 0 ? longest : 1;
-  if (2 * units * s.row_tiles <= kvq::kComputeUnits) {   // (of a causal chunk, row tiles have more keys the later they are)
+  if (small && shared) {
+    const int64_t share = 2 * kvq::kComputeUnits / units;
+    s.most = (longest + share - 1) / share;
+  } else if (2 * units * s.row_tiles <= kvq::kComputeUnits) {   // (of a causal chunk, row tiles have more keys the later they are)
     const int64_t work = units * (s.row_tiles * held + s.row_tiles * (own + 1) / 2);
     s.most = (work + kvq::kComputeUnits - 1) / kvq::kComputeUnits;
     if (s.most < 2) s.most = 2;

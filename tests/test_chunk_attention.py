@@ -132,6 +132,13 @@ def test_many_sequences_with_few_rows(bits, group_k, group_v, paged):
     run(cfg, hist, [1 + b % 31 for b in range(64)], paged, scale=0.2, sequences=[0, 1, 2, 61, 62], heads=[0, 3])
 
 
+@pytest.mark.parametrize("q_heads,kv_heads,new", [(32, 32, [5, 0, 128]), (128, 32, [32, 1, 9]), (40, 40, [1, 1, 1])])
+def test_few_rows_of_many_units_share_their_keys(q_heads, kv_heads, new):
+    """Two small workgroups per compute unit, each with a part of a unit's keys."""
+    cfg = H.config(1, 3, q_heads, kv_heads, 2048)
+    run(cfg, [1700, 1650, 800], new, paged=True, heads=[0, 17, kv_heads - 1])
+
+
 @pytest.mark.parametrize("batch,kv_heads,most", [(40, 16, 40), (24, 16, 300), (64, 24, 3)])
 def test_many_sequences_of_different_lengths(batch, kv_heads, most):
     """More workgroups than the device takes at once, dealt by the sequences' work."""
