@@ -863,13 +863,18 @@ bool rows_ok(const void* p, int64_t stride, int64_t heads, int64_t head_dim) {
 //    there are compute units, two tiles of 64 keys each at least (4 tokens over 8000, 32 / 8 heads: 193 us with one workgroup each,
 //    36 / 27 / 20 / 28 with 16 / 11 / 4 / 2 tiles each; 33 tokens of 4 sequences 55 with 16 tiles each, 70 with 11).  With more row
 //    tiles than that it costs more than it gives: a workgroup that has a compute unit to itself is nearly as fast as two that
-//    share one (a prompt of 1000 tokens: 30 us, 36 with two workgroups each).
+//    share one (a prompt of 1000 tokens: 30 us, 36 with two workgroups each), except where rounds of workgroups would be left half
+//    empty over a long cache (`full`: every sequence has max_tokens tokens; of others the host does not know the row tiles).
+//    Two or three workgroups each are weighed by the rounds, a tile of keys taken for 2.3 us, a workgroup's beginning and end for
+//    three tiles, and the shares' way to memory and back (us, one / two / three: 4 x 580 tokens over 4000, 320 row tiles, 324 /
+//    300 / 296, over 8000 573 / 495 / 496; 10 x 256 over 6000 460 / 412 / 400; 4 x 300 over 4000, 160 row tiles, 171 / 170 /
+//    156; 4 x 700 over 4000, 352, 340 / 318 / 371; 4 x 580 over 2000 185 / 183 / 193).
 struct ChunkShape {
   int32_t waves;
   int64_t row_tiles, most, splits;
   int64_t unit_rows() const { return row_tiles * waves * kvq::kChunkWaveRows; }
 };
-ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quant, int64_t n_res, bool with_new) {
+ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quant, int64_t n_res, bool with_new, bool full) {
   const int64_t units = (int64_t)cfg->batch * cfg->kv_heads, unit_rows = max_tokens * (cfg->q_heads / cfg->kv_heads);
   auto tiles_of = [&](int64_t waves) { return (unit_rows + waves * kvq::kChunkWaveRows - 1) / (waves * kvq::kChunkWaveRows); };
   ChunkShape s;
@@ -889,6 +894,16 @@ ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quan
     const int64_t work = units * (s.row_tiles * held + s.row_tiles * (own + 1) / 2);
     s.most = (work + kvq::kComputeUnits - 1) / kvq::kComputeUnits;
     if (s.most < 2) s.most = 2;
+  } else if (full && s.waves == 8 && held >= 4 * own && units * s.row_tiles < 2 * kvq::kComputeUnits) {
+    double least = 0.0;
+    for (int64_t n = 1; n <= 3; ++n) {
+      const int64_t each = (longest + n - 1) / n, rounds = (units * s.row_tiles * n + kvq::kComputeUnits - 1) / kvq::kComputeUnits;
+      const double shares = n > 1 ? 4.0 + 2.0 * n * units * unit_rows * (cfg->head_dim + 2) * 4 / 3.5e6 : 0.0;
+      const double cost = rounds * (each + 3) * 2.3 + shares;
+      if (n > 1 && cost >= least) continue;
+      least = cost;
+      s.most = each;
+    }
   }
   s.splits = (longest + s.most - 1) / s.most;
   if (s.splits < 1) s.splits = 1;
@@ -906,9 +921,12 @@ int64_t kvq_prompt_workspace_bytes(const kvq_config* cfg, int32_t max_tokens, in
   if (st != KVQ_OK) return st;
   if (max_tokens < 1 || n_quant < 0 || n_quant > cfg->max_seq || n_quant % cfg->group_k != 0) return KVQ_ERR_INVALID_ARG;
   if (n_res < 0 || n_res > (int32_t)res_rows_of(cfg)) return KVQ_ERR_INVALID_ARG;
-  const int64_t with = chunk_workspace_bytes(cfg, chunk_shape(cfg, max_tokens, n_quant, n_res, true));
-  const int64_t without = chunk_workspace_bytes(cfg, chunk_shape(cfg, max_tokens, n_quant, n_res, false));
-  return with > without ? with : without;
+  int64_t most = 0;                                      // with new tokens or without, with lengths that are all the same or not
+  for (int i = 0; i < 4; ++i) {
+    const int64_t need = chunk_workspace_bytes(cfg, chunk_shape(cfg, max_tokens, n_quant, n_res, i & 1, i & 2));
+    most = need > most ? need : most;
+  }
+  return most;
 }
 
 int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q, int64_t q_stride, const void* k_new,
@@ -938,7 +956,8 @@ int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q
     return KVQ_ERR_INVALID_ARG;
   if (((uintptr_t)qc.mask) & 3) return KVQ_ERR_INVALID_ARG;
   const int64_t g = cfg->q_heads / cfg->kv_heads;
-  const ChunkShape shape = chunk_shape(cfg, chunk.max_tokens, n_quant, n_res, k_new != nullptr);
+  const ChunkShape shape = chunk_shape(cfg, chunk.max_tokens, n_quant, n_res, k_new != nullptr,
+                                        !chunk.starts || chunk.total == (int64_t)cfg->batch * chunk.max_tokens);
   const int64_t units = (int64_t)cfg->batch * cfg->kv_heads, items = units * shape.row_tiles * shape.splits;
   int32_t parts = 1;
   while (units * parts % 8) parts *= 2;

@@ -139,6 +139,12 @@ def test_few_rows_of_many_units_share_their_keys(q_heads, kv_heads, new):
     run(cfg, [1700, 1650, 800], new, paged=True, heads=[0, 17, kv_heads - 1])
 
 
+def test_rounds_that_would_be_half_empty():
+    """144 row tiles over a long cache, three workgroups each."""
+    cfg = H.config(1, 3, 48, 48, 8192)
+    run(cfg, [8000, 7900, 5000], [250] * 3, heads=[0, 47], sequences=[0, 2])
+
+
 @pytest.mark.parametrize("batch,kv_heads,most", [(40, 16, 40), (24, 16, 300), (64, 24, 3)])
 def test_many_sequences_of_different_lengths(batch, kv_heads, most):
     """More workgroups than the device takes at once, dealt by the sequences' work."""
