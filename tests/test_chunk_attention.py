@@ -127,9 +127,9 @@ def test_enough_rows_for_one_workgroup_each(batch, tokens):
 @pytest.mark.parametrize("paged", [False, True])
 def test_many_sequences_with_few_rows(bits, group_k, group_v, paged):
     """The units alone fill the device: workgroups of four wavefronts, each a half of a block's codes."""
-    cfg = H.config(1, 64, 8, 4, 512, bits=bits, group_k=group_k, group_v=group_v, residual=40)
-    hist = [450 - 5 * b if b % 3 else 0 for b in range(64)]
-    run(cfg, hist, [1 + b % 31 for b in range(64)], paged, scale=0.2, sequences=[0, 1, 2, 61, 62], heads=[0, 3])
+    cfg = H.config(1, 66, 8, 4, 512, bits=bits, group_k=group_k, group_v=group_v, residual=40)
+    hist = [450 - 5 * b if b % 3 else 0 for b in range(66)]
+    run(cfg, hist, [1 + b % 31 for b in range(66)], paged, scale=0.2, sequences=[0, 1, 2, 61, 64], heads=[0, 3])
 
 
 @pytest.mark.parametrize("q_heads,kv_heads,new", [(32, 32, [5, 0, 128]), (128, 32, [32, 1, 9]), (40, 40, [1, 1, 1])])
