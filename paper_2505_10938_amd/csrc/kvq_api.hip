@@ -860,9 +860,9 @@ bool rows_ok(const void* p, int64_t stride, int64_t heads, int64_t head_dim) {
 //    20 42 / 36); and where nothing is quantized and there are at most two rounds of the larger workgroups (prompts of 300
 //    tokens 19.5 / 21.9, 1000 31 / 47, 2 x 2000 with 32 kv heads 118 / 133; 4000 155 / 153).
 //  - A row tile's keys are shared out where there are at most half as many row tiles as compute units, to as many workgroups as
-//    there are compute units, two tiles of 64 keys each at least (4 tokens over 8000, 32 / 8 heads: 193 us with one workgroup each,
-//    36 / 27 / 20 / 28 with 16 / 11 / 4 / 2 tiles each; 33 tokens of 4 sequences 55 with 16 tiles each, 70 with 11).  With more row
-//    tiles than that it costs more than it gives: a workgroup that has a compute unit to itself is nearly as fast as two that
+//    there are compute units (32 / 8 heads, 4 tokens over 8000: 193 us with one workgroup each, 36 / 27 / 20 with 16 / 11 / 4 tiles
+//    of 64 keys each; a token over 300 11.4 with one tile each, 14.3 with two; 9 over 1003 14.7, 15.8; 64 over 500 22.8, 21.9).
+//    With more row tiles than that it costs more than it gives: a workgroup that has a compute unit to itself is nearly as fast as two that
 //    share one (a prompt of 1000 tokens: 30 us, 36 with two workgroups each), except where rounds of workgroups would be left half
 //    empty over a long cache (`full`: every sequence has max_tokens tokens; of others the host does not know the row tiles).
 //    Two or three workgroups each are weighed by the rounds, a tile of keys taken for 2.3 us, a workgroup's beginning and end for
@@ -893,7 +893,6 @@ ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quan
   } else if (2 * units * s.row_tiles <= kvq::kComputeUnits) {   // (of a causal chunk, row tiles have more keys the later they are)
     const int64_t work = units * (s.row_tiles * held + s.row_tiles * (own + 1) / 2);
     s.most = (work + kvq::kComputeUnits - 1) / kvq::kComputeUnits;
-    if (s.most < 2) s.most = 2;
   } else if (full && s.waves == 8 && held >= 4 * own && units * s.row_tiles < 2 * kvq::kComputeUnits) {
     double least = 0.0;
     for (int64_t n = 1; n <= 3; ++n) {

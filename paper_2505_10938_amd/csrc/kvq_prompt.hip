@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(64 * NW, 2) prompt_attention_kernel(ChunkArgs 
   const int nq = held.nq, rs = held.rs, n_pool = held.n_pool, n_aux = held.n_aux;
   const int n_rows = n_pool + n_aux + held.nr;           // full-precision rows of the cache
   const TileKeys keys = tile_keys(a, held, n, first_row, live_rows);
-  const int first_token = first_row >> a.g_shift, n_new = keys.n_new, tq = keys.tq, ti = keys.ti, tr = keys.tr;
+  const int n_new = keys.n_new, tq = keys.tq, ti = keys.ti, tr = keys.tr;
   const int my_splits = keys.splits;
   if (split >= my_splits) return;
   const int per = (keys.tiles + my_splits - 1) / my_splits;
