@@ -864,17 +864,19 @@ bool rows_ok(const void* p, int64_t stride, int64_t heads, int64_t head_dim) {
 //    of 64 keys each; a token over 300 11.4 with one tile each, 14.3 with two; 9 over 1003 14.7, 15.8; 64 over 500 22.8, 21.9).
 //    With more row tiles than that it costs more than it gives: a workgroup that has a compute unit to itself is nearly as fast as two that
 //    share one (a prompt of 1000 tokens: 30 us, 36 with two workgroups each), except where rounds of workgroups would be left half
-//    empty over a long cache (`full`: every sequence has max_tokens tokens; of others the host does not know the row tiles).
+//    empty over a long cache.  (`total` new tokens: of sequences of different lengths the host knows only how many row tiles
+//    they have at most.  0: of any lengths, for the size of the workspace.)
 //    Two or three workgroups each are weighed by the rounds, a tile of keys taken for 2.3 us, a workgroup's beginning and end for
 //    three tiles, and the shares' way to memory and back (us, one / two / three: 4 x 580 tokens over 4000, 320 row tiles, 324 /
 //    300 / 296, over 8000 573 / 495 / 496; 10 x 256 over 6000 460 / 412 / 400; 4 x 300 over 4000, 160 row tiles, 171 / 170 /
-//    156; 4 x 700 over 4000, 352, 340 / 318 / 371; 4 x 580 over 2000 185 / 183 / 193).
+//    156; 4 x 700 over 4000, 352, 340 / 318 / 371; 4 x 580 over 2000 185 / 183 / 193; of different lengths, one or what is
+//    chosen: 4 of up to 300 over up to 4000 152 / 75, 16 of up to 100 over 2000 87 / 66, 8 of up to 200 over 3000 122 / 77).
 struct ChunkShape {
   int32_t waves;
   int64_t row_tiles, most, splits;
   int64_t unit_rows() const { return row_tiles * waves * kvq::kChunkWaveRows; }
 };
-ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quant, int64_t n_res, bool with_new, bool full) {
+ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quant, int64_t n_res, bool with_new, int64_t total) {
   const int64_t units = (int64_t)cfg->batch * cfg->kv_heads, unit_rows = max_tokens * (cfg->q_heads / cfg->kv_heads);
   auto tiles_of = [&](int64_t waves) { return (unit_rows + waves * kvq::kChunkWaveRows - 1) / (waves * kvq::kChunkWaveRows); };
   ChunkShape s;
@@ -893,13 +895,16 @@ ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quan
   } else if (2 * units * s.row_tiles <= kvq::kComputeUnits) {   // (of a causal chunk, row tiles have more keys the later they are)
     const int64_t work = units * (s.row_tiles * held + s.row_tiles * (own + 1) / 2);
     s.most = (work + kvq::kComputeUnits - 1) / kvq::kComputeUnits;
-  } else if (full && s.waves == 8 && held >= 4 * own && units * s.row_tiles < 2 * kvq::kComputeUnits) {
+  } else if (s.waves == 8 && held >= 4 * own && units * s.row_tiles < 2 * kvq::kComputeUnits) {
+    const int64_t rows = total * cfg->q_heads, g = cfg->q_heads / cfg->kv_heads;
+    int64_t tiles = cfg->kv_heads * (total * g / (s.waves * kvq::kChunkWaveRows) + cfg->batch);
+    if (tiles > units * s.row_tiles) tiles = units * s.row_tiles;
     double least = 0.0;
-    for (int64_t n = 1; n <= 3; ++n) {
-      const int64_t each = (longest + n - 1) / n, rounds = (units * s.row_tiles * n + kvq::kComputeUnits - 1) / kvq::kComputeUnits;
-      const double shares = n > 1 ? 4.0 + 2.0 * n * units * unit_rows * (cfg->head_dim + 2) * 4 / 3.5e6 : 0.0;
+    for (int64_t n = total > 0 ? 1 : 3; n <= 3; ++n) {
+      const int64_t each = (longest + n - 1) / n, rounds = (tiles * n + kvq::kComputeUnits - 1) / kvq::kComputeUnits;
+      const double shares = n > 1 ? 4.0 + 2.0 * n * rows * (cfg->head_dim + 2) * 4 / 3.5e6 : 0.0;
       const double cost = rounds * (each + 3) * 2.3 + shares;
-      if (n > 1 && cost >= least) continue;
+      if (least > 0.0 && cost >= least) continue;
       least = cost;
       s.most = each;
     }
@@ -920,12 +925,9 @@ int64_t kvq_prompt_workspace_bytes(const kvq_config* cfg, int32_t max_tokens, in
   if (st != KVQ_OK) return st;
   if (max_tokens < 1 || n_quant < 0 || n_quant > cfg->max_seq || n_quant % cfg->group_k != 0) return KVQ_ERR_INVALID_ARG;
   if (n_res < 0 || n_res > (int32_t)res_rows_of(cfg)) return KVQ_ERR_INVALID_ARG;
-  int64_t most = 0;                                      // with new tokens or without, with lengths that are all the same or not
-  for (int i = 0; i < 4; ++i) {
-    const int64_t need = chunk_workspace_bytes(cfg, chunk_shape(cfg, max_tokens, n_quant, n_res, i & 1, i & 2));
-    most = need > most ? need : most;
-  }
-  return most;
+  const int64_t with = chunk_workspace_bytes(cfg, chunk_shape(cfg, max_tokens, n_quant, n_res, true, 0));
+  const int64_t without = chunk_workspace_bytes(cfg, chunk_shape(cfg, max_tokens, n_quant, n_res, false, 0));
+  return with > without ? with : without;
 }
 
 int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q, int64_t q_stride, const void* k_new,
@@ -955,8 +957,7 @@ int32_t kvq_prompt_attention(const kvq_config* cfg, int32_t layer, const void* q
     return KVQ_ERR_INVALID_ARG;
   if (((uintptr_t)qc.mask) & 3) return KVQ_ERR_INVALID_ARG;
   const int64_t g = cfg->q_heads / cfg->kv_heads;
-  const ChunkShape shape = chunk_shape(cfg, chunk.max_tokens, n_quant, n_res, k_new != nullptr,
-                                        !chunk.starts || chunk.total == (int64_t)cfg->batch * chunk.max_tokens);
+  const ChunkShape shape = chunk_shape(cfg, chunk.max_tokens, n_quant, n_res, k_new != nullptr, chunk.total);
   const int64_t units = (int64_t)cfg->batch * cfg->kv_heads, items = units * shape.row_tiles * shape.splits;
   int32_t parts = 1;
   while (units * parts % 8) parts *= 2;

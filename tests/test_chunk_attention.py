@@ -145,6 +145,13 @@ def test_rounds_that_would_be_half_empty():
     run(cfg, [8000, 7900, 5000], [250] * 3, heads=[0, 47], sequences=[0, 2])
 
 
+@pytest.mark.parametrize("new", [[300, 20, 1, 0], [1, 0, 299, 300], [1, 0, 0, 0]])
+def test_one_long_chunk_among_short_ones(new):
+    """The host knows the sum of the lengths, and shares keys out by it."""
+    cfg = H.config(1, 4, 32, 8, 4096)
+    run(cfg, [3900, 2500, 900, 4000], new, paged=True, heads=[0, 5])
+
+
 @pytest.mark.parametrize("batch,kv_heads,most", [(40, 16, 40), (24, 16, 300), (64, 24, 3)])
 def test_many_sequences_of_different_lengths(batch, kv_heads, most):
     """More workgroups than the device takes at once, dealt by the sequences' work."""
