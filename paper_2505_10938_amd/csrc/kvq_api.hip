@@ -862,6 +862,8 @@ bool rows_ok(const void* p, int64_t stride, int64_t heads, int64_t head_dim) {
 //  - A row tile's keys are shared out where there are at most half as many row tiles as compute units, to as many workgroups as
 //    there are compute units (32 / 8 heads, 4 tokens over 8000: 193 us with one workgroup each, 36 / 27 / 20 with 16 / 11 / 4 tiles
 //    of 64 keys each; a token over 300 11.4 with one tile each, 14.3 with two; 9 over 1003 14.7, 15.8; 64 over 500 22.8, 21.9).
+//    Of sequences of different lengths the row tiles are estimated from their sum, a third of the most at least, which the
+//    workspace has room for (4 of up to 100 tokens over up to 8000 92 -> 80 us, 2 of up to 300 over 4000, 4 kv heads, 117 -> 93).
 //    With more row tiles than that it costs more than it gives: a workgroup that has a compute unit to itself is nearly as fast as two that
 //    share one (a prompt of 1000 tokens: 30 us, 36 with two workgroups each), except where rounds of workgroups would be left half
 //    empty over a long cache.  (`total` new tokens: of sequences of different lengths the host knows only how many row tiles
@@ -889,16 +891,19 @@ ChunkShape chunk_shape(const kvq_config* cfg, int64_t max_tokens, int64_t n_quan
   s.waves = small || prompt ? 4 : 8;
   s.row_tiles = tiles_of(s.waves);
   s.most = longest > 0 ? longest : 1;
+  const int64_t at_most = units * s.row_tiles, g = cfg->q_heads / cfg->kv_heads;
+  int64_t tiles = cfg->kv_heads * (total * g / (s.waves * kvq::kChunkWaveRows) + cfg->batch);
+  if (tiles > at_most) tiles = at_most;
   if (small && shared) {
     const int64_t share = 2 * kvq::kComputeUnits / units;
     s.most = (longest + share - 1) / share;
-  } else if (2 * units * s.row_tiles <= kvq::kComputeUnits) {   // (of a causal chunk, row tiles have more keys the later they are)
-    const int64_t work = units * (s.row_tiles * held + s.row_tiles * (own + 1) / 2);
+  } else if (2 * at_most <= kvq::kComputeUnits) {
+    const int64_t third = (at_most + 2) / 3, live = total > 0 && tiles > third ? tiles : third;
+    const int64_t work = live * held + live * (own + 1) / 2;    // (of a causal chunk, row tiles have more keys the later they are)
     s.most = (work + kvq::kComputeUnits - 1) / kvq::kComputeUnits;
-  } else if (s.waves == 8 && held >= 4 * own && units * s.row_tiles < 2 * kvq::kComputeUnits) {
-    const int64_t rows = total * cfg->q_heads, g = cfg->q_heads / cfg->kv_heads;
-    int64_t tiles = cfg->kv_heads * (total * g / (s.waves * kvq::kChunkWaveRows) + cfg->batch);
-    if (tiles > units * s.row_tiles) tiles = units * s.row_tiles;
+    if (s.most < 1) s.most = 1;
+  } else if (s.waves == 8 && held >= 4 * own && at_most < 2 * kvq::kComputeUnits) {
+    const int64_t rows = total * cfg->q_heads;
     double least = 0.0;
     for (int64_t n = total > 0 ? 1 : 3; n <= 3; ++n) {
       const int64_t each = (longest + n - 1) / n, rounds = (tiles * n + kvq::kComputeUnits - 1) / kvq::kComputeUnits;
